@@ -421,7 +421,8 @@ def kernel_model(name, cfg, elem, recompute=False):
     name = name[3:] + "_kernel" if small else name.replace("_narrow", "_kernel")
     flops = {"g1_kernel": nb * g * runs, "g2_kernel": g, "g2h_kernel": g,
              "g3_kernel": g, "g3h_kernel": g,
-             "g4_kernel": g, "g5_kernel": nb * g, "g6_kernel": nb * g}
+             "g4_kernel": g, "g5_kernel": nb * g, "g6_kernel": nb * g,
+             "mx_tile": (nb + 1) * g}   # both products of 4-bit experts
     if small:
         # the weights of the experts with tokens read once, the rows in and out;
         # whichever bound is the longer
@@ -455,6 +456,18 @@ def kernel_model(name, cfg, elem, recompute=False):
         "rb_dwg_partial": T * E * 4 + T * d * elem,            # float32
         "rb_products": 2 * T * E * 4 + E * d * elem + 3 * T * d * elem,
         "rb_dwg_reduce": 0,
+        # around the layer: block norms, the experts' gradients' norm and clipping, 4-bit
+        # weights and rows (one layer of cfg)
+        "norm_fwd": 4 * T * d * elem,
+        "norm_bwd": 6 * T * d * elem,
+        "norm_bwd_sum": 3 * 512 * d * 4,
+        "grad_sumsq": 3 * E * d * f * 4,
+        "grad_sum_parts": 2048 * 8,
+        "grad_scale": 2 * 3 * E * d * f * 4,
+        "mx_quantize": T * d * (elem + 17 / 32),
+        "mx_quantize_transposed": 3 * E * d * f * (elem + 17 / 32),
+        "mx_dequantize": T * d * (elem + 17 / 32),
+        "mx_stream": 3 * E * (1.0 - (1.0 - k / E) ** T) * d * f * 17 / 32,
     }
     return float(byts.get(name, 0)), "GB/s", "hbm"
 

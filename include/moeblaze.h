@@ -97,6 +97,13 @@ extern "C" {
  * depend on their order). bfloat16 only: with MOE_F32, MOE_ERR_UNSUPPORTED.
  * Every other call rejects it (MOE_ERR_INVALID_ARG). */
 #define MOE_ATOMIC_COMBINE 128u
+/* Flags of the operators around the layer; every other call rejects them. */
+#define MOE_NORM_POST    256u   /* moe_norm_*: the block's output is normalised */
+#define MOE_NORM_PRE     512u   /* moe_norm_*: the next block's input is produced */
+#define MOE_GATE_CHANNEL 1024u  /* moe_norm_*: a gate per channel [d] ... */
+#define MOE_GATE_TOKEN   2048u  /* ... per token [T]; with both flags, [T, d] */
+#define MOE_TRANSPOSED   4096u  /* moe_mx_quantize: src is [batch, K, R] */
+#define MOE_GATED        8192u  /* moe_mx_gemm: SiLU(x w) * (x w3) */
 
 /* Human-readable name of a status code (static storage). */
 const char* moe_strerror(int status);
@@ -321,6 +328,121 @@ int moe_route_bwd(const float* d_gates, const float* logits, const int32_t* topk
                   int64_t T, int d, int E, int k, unsigned flags,
                   float* dw_gate, void* dx, void* workspace, size_t workspace_bytes,
                   hipStream_t stream);
+
+/*
+ * moe_norm_fwd -- the tail of one residual block and the head of the next, in one
+ * pass: post-norm of the block's output y, its gate, the residual scale and the
+ * addition, then the pre-norm that makes the next block's input. Per row of d:
+ *   p = y / sqrt(mean(y^2) + eps) * w_post     (MOE_NORM_POST; else p = y)
+ *   r = res_scale * res + gate * p             (gate: see below; else 1)
+ *   n = r / sqrt(mean(r^2) + eps) * w_pre      (MOE_NORM_PRE)
+ * n is computed from r before r is rounded. Without a block output (y NULL) it
+ * is the pre-norm of res alone: n from r = res, which is not written again.
+ * In:  res [T,d]; y [T,d] or NULL; gate [d] (MOE_GATE_CHANNEL), [T]
+ *      (MOE_GATE_TOKEN), [T,d] (both flags) or NULL (neither); w_post, w_pre [d]
+ *      with their flags, else NULL (element type per flags, all of them).
+ * Out: r [T,d] (NULL without y), n [T,d] (MOE_NORM_PRE, else NULL), rstd_post,
+ *      rstd_pre [T] float32 (the reciprocal deviations, which the backward takes;
+ *      each may be NULL).
+ * r may be res or y, and n may be y or res: a row is read before it is written.
+ * Other overlaps are not allowed. Squares are float32: |values| above 1e18
+ * overflow them. Limits: d a multiple of 8, d <= 8192; eps > 0; without y,
+ * res_scale 1 and neither MOE_NORM_POST nor a gate.
+ *
+ * moe_norm_bwd -- its gradient. With G = dr + (the gradient through n):
+ *   dres = res_scale * G,  dy, dgate, dw_post, dw_pre as the chain rule gives them.
+ * In:  dr [T,d] (gradient of r; NULL: nothing but n used r), dn [T,d] (of n;
+ *      MOE_NORM_PRE), y [T,d] (with MOE_NORM_POST or a gate, else it may be
+ *      NULL), r [T,d] as the forward wrote it (MOE_NORM_PRE; without a block
+ *      output: res), gate, w_post, w_pre, rstd_post, rstd_pre as in the forward.
+ * Out: dres [T,d]; dy [T,d] (NULL: no block output); dgate: [d] or [T] float32,
+ *      or [T,d] (element type per flags); dw_post, dw_pre [d] float32. With
+ *      T == 0 the [d] sums are written as zeros and nothing else happens.
+ * dres and dy may take the place of any of dr, dn, y and r (not each other's).
+ * Deterministic. workspace: moe_norm_bwd_workspace_size(T,d,flags) bytes.
+ */
+int moe_norm_fwd(const void* res, const void* y, const void* gate, const void* w_post,
+                 const void* w_pre, float res_scale, float eps, int64_t T, int d,
+                 unsigned flags, void* r, void* n, float* rstd_post, float* rstd_pre,
+                 hipStream_t stream);
+size_t moe_norm_bwd_workspace_size(int64_t T, int d, unsigned flags);
+int moe_norm_bwd(const void* dr, const void* dn, const void* y, const void* r, const void* gate,
+                 const void* w_post, const void* w_pre, const float* rstd_post,
+                 const float* rstd_pre, float res_scale, int64_t T, int d, unsigned flags,
+                 void* dres, void* dy, void* dgate, float* dw_post, float* dw_pre,
+                 void* workspace, size_t workspace_bytes, hipStream_t stream);
+
+/*
+ * moe_grad_norm -- the sum of squares, and the norm, of a list of tensors:
+ *   *sumsq = sum over all elements of g^2 (64-bit),  *norm = sqrt(*sumsq).
+ * The squares are 64-bit, and the sum is taken in a fixed order (deterministic).
+ * Where a model's gradients are spread over several devices, the devices' sumsq
+ * add up to the whole's.
+ * In:  grads: HOST array of n device pointers, aligned to their elements; sizes:
+ *      host array of their element counts (0 allowed); types: host array of
+ *      MOE_BF16 or MOE_F32 each. The three arrays are read before the call returns.
+ * Out: sumsq (double) and norm (float32) on the device. n == 0 gives zeros.
+ * workspace: moe_grad_norm_workspace_size(n) bytes.
+ *
+ * moe_grad_clip -- out[i] = c * grads[i] with
+ *   c = min(1, max_norm / (sqrt(*sumsq) + 1e-6))   (sumsq on the device),
+ * so that the list's norm is at most max_norm. A NaN in sumsq makes c and every
+ * output NaN; an infinite one makes c zero. outs NULL: in place, and with c == 1
+ * nothing is read or written. Else each out tensor is its gradient itself or
+ * overlaps no tensor of the call (MOE_ERR_INVALID_ARG, as for two gradients that
+ * overlap while one is written). max_norm >= 0 (infinity: c = 1).
+ */
+size_t moe_grad_norm_workspace_size(int n);
+int moe_grad_norm(const void* const* grads, const int64_t* sizes, const unsigned* types, int n,
+                  double* sumsq, float* norm, void* workspace, size_t workspace_bytes,
+                  hipStream_t stream);
+int moe_grad_clip(const void* const* grads, void* const* outs, const int64_t* sizes,
+                  const unsigned* types, int n, const double* sumsq, double max_norm,
+                  hipStream_t stream);
+
+/*
+ * moe_mx_quantize -- microscaled 4-bit floating point (OCP Microscaling MXFP4):
+ * each 32 values along K share a scale 2^(s - 127) with
+ *   s - 127 = floor(log2(largest magnitude)) - 2   (at least -127),
+ * and become e2m1 codes (0, 0.5, 1, 1.5, 2, 3, 4, 6 and their negatives) of
+ * value / scale: to nearest, ties to the even code, beyond 6 to 6. Value 2i of a
+ * block is the low half of its byte i. A block that holds an infinity or a NaN
+ * gets s = 255 (NaN: all of its values).
+ * In:  src [batch, R, K], or with MOE_TRANSPOSED [batch, K, R] (the layout of
+ *      w1, w3, w2: K is the axis that a product sums over); MOE_F32 / MOE_BF16.
+ * Out: codes [batch, R, K/2] bytes, scales [batch, R, K/32] bytes.
+ * K a multiple of 32; MOE_TRANSPOSED: R even, batch <= 65535; fewer than 2^36 values.
+ *
+ * moe_mx_dequantize -- out [R, K] = the values of codes [R, K/2] under scales
+ * [R, K/32] (any bytes), bfloat16 or MOE_F32.
+ */
+int moe_mx_quantize(const void* src, int64_t batch, int64_t R, int K, unsigned flags,
+                    void* codes, void* scales, hipStream_t stream);
+int moe_mx_dequantize(const void* codes, const void* scales, int64_t R, int K, unsigned flags,
+                      void* out, hipStream_t stream);
+
+/*
+ * moe_mx_gemm -- products grouped by expert with ragged row counts, the weights
+ * held in microscaled 4 bits. For each slot s of expert e (offsets[e] <= s <
+ * offsets[e+1]) with row t = rows[s] (rows NULL: t = s):
+ *   out[s] = x[t] w[e]^T                       (no flag)
+ *   out[s] = SiLU or ReLU of it                (MOE_ACT_SILU, MOE_ACT_RELU)
+ *   out[s] = SiLU(x[t] w[e]^T) * x[t] w3[e]^T  (MOE_GATED)
+ * accumulated in float32, the activation taken there, and rounded once: the two
+ * products of an expert FFN at inference, the forward of one layer being
+ * moe_route, moe_build_index, this with rows = expert_token_indices, this with
+ * rows NULL, and moe_combine.
+ * In:  x [T,K] bfloat16 (x_scales NULL), or codes [T,K/2] with x_scales [T,K/32]
+ *      as moe_mx_quantize writes them; w, w3 [E,N,K/2] codes, w_scales, w3_scales
+ *      [E,N,K/32] (w3 with MOE_GATED, else NULL); offsets [E+1], rows [S] int32.
+ * Out: out [S,N] bfloat16. Rows at or behind offsets[E] are left as they were.
+ * Limits: K and N multiples of 64, E <= 256, S < 2^31, T < 2^31; rows NULL: T == S.
+ * The scales 0 to 254 stand for 2^(s - 127), 255 for NaN. No workspace.
+ */
+int moe_mx_gemm(const void* x, const void* x_scales, const void* w, const void* w_scales,
+                const void* w3, const void* w3_scales, const int32_t* offsets,
+                const int32_t* rows, int64_t T, int64_t S, int K, int N, int E, unsigned flags,
+                void* out, hipStream_t stream);
 
 /*
  * Kernel timing probe (diagnostics; not needed for computing anything, and

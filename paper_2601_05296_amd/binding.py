@@ -31,6 +31,12 @@ MOE_ACT_RELU = 16
 MOE_H_ON_LOAD = 32
 MOE_ACCUMULATE_DW = 64
 MOE_ATOMIC_COMBINE = 128
+MOE_NORM_POST = 256
+MOE_NORM_PRE = 512
+MOE_GATE_CHANNEL = 1024
+MOE_GATE_TOKEN = 2048
+MOE_TRANSPOSED = 4096
+MOE_GATED = 8192
 ACT_FLAG = {"swiglu": 0, "silu": MOE_ACT_SILU, "relu": MOE_ACT_RELU}
 
 # Every symbol declared in include/moeblaze.h.
@@ -39,7 +45,10 @@ EXPORTS = ("moe_strerror", "moe_last_error", "moe_route", "moe_build_index_works
            "moe_ffn_bwd", "moe_ffn_recompute", "moe_ffn_fwd_combine_workspace_size",
            "moe_ffn_fwd_combine",
            "moe_ffn_bwd_combine_workspace_size", "moe_ffn_bwd_combine",
-           "moe_route_bwd_workspace_size", "moe_route_bwd", "moe_probe_enable",
+           "moe_route_bwd_workspace_size", "moe_route_bwd", "moe_norm_fwd",
+           "moe_norm_bwd_workspace_size", "moe_norm_bwd", "moe_grad_norm_workspace_size",
+           "moe_grad_norm", "moe_grad_clip", "moe_mx_quantize", "moe_mx_dequantize",
+           "moe_mx_gemm", "moe_probe_enable",
            "moe_probe_disable", "moe_probe_count", "moe_probe_dropped", "moe_probe_get")
 
 
@@ -67,6 +76,7 @@ def load_library(path: str = LIB):
                           "`python -m paper_2601_05296_amd.build`" % path)
     lib = ctypes.CDLL(path)
     P, I64, I, U, SZ = ctypes.c_void_p, ctypes.c_int64, ctypes.c_int, ctypes.c_uint, ctypes.c_size_t
+    F = ctypes.c_float
     sig = {
         "moe_strerror": (ctypes.c_char_p, [I]),
         "moe_last_error": (ctypes.c_char_p, []),
@@ -86,6 +96,15 @@ def load_library(path: str = LIB):
         "moe_ffn_bwd_combine": (I, [P] * 12 + [I64, I, I, I, I, U] + [P] * 6 + [SZ, P]),
         "moe_route_bwd_workspace_size": (SZ, [I64, I, I, I, U]),
         "moe_route_bwd": (I, [P] * 6 + [I64, I, I, I, U, P, P, P, SZ, P]),
+        "moe_norm_fwd": (I, [P] * 5 + [F, F, I64, I, U] + [P] * 5),
+        "moe_norm_bwd_workspace_size": (SZ, [I64, I, U]),
+        "moe_norm_bwd": (I, [P] * 9 + [F, I64, I, U] + [P] * 6 + [SZ, P]),
+        "moe_grad_norm_workspace_size": (SZ, [I]),
+        "moe_grad_norm": (I, [P, P, P, I, P, P, P, SZ, P]),
+        "moe_grad_clip": (I, [P, P, P, P, I, P, ctypes.c_double, P]),
+        "moe_mx_quantize": (I, [P, I64, I64, I, U, P, P, P]),
+        "moe_mx_dequantize": (I, [P, P, I64, I, U, P, P]),
+        "moe_mx_gemm": (I, [P] * 8 + [I64, I64, I, I, I, U, P, P]),
         "moe_probe_enable": (I, [I]),
         "moe_probe_disable": (None, []),
         "moe_probe_count": (I, []),
@@ -363,6 +382,148 @@ def moe_route_bwd(d_gates, logits, topk_ids, gates, x, w_gate, T, d, E, k, flags
                                         _ptr(gates), _ptr(x), _ptr(w_gate), T, d, E, k, flags,
                                         _ptr(dw_gate), _ptr(dx), _ptr(workspace),
                                         workspace_bytes, _stream(stream)))
+
+
+def _here(*tensors):
+    """The tensors of a call have to be on torch's current device: the call goes to that
+    device's stream."""
+    dev = None
+    for t in tensors:
+        if t is None or isinstance(t, int):
+            continue
+        if dev is None:
+            if not t.is_cuda:
+                raise ValueError("tensor must be on the GPU")
+            dev = torch.cuda.current_device()
+        if t.get_device() != dev:
+            raise ValueError("tensor on %s, the current device is cuda:%d" % (t.device, dev))
+
+
+def _gate_count(flags, T, d):
+    """Elements of the gate of a norm call under `flags` (0: no gate)."""
+    kind = flags & (MOE_GATE_CHANNEL | MOE_GATE_TOKEN)
+    return {0: 0, MOE_GATE_CHANNEL: d, MOE_GATE_TOKEN: T}.get(kind, T * d)
+
+
+def moe_norm_fwd(res, y, gate, w_post, w_pre, res_scale, eps, T, d, flags, r, n, rstd_post=None,
+                 rstd_pre=None, stream=None):
+    el, f32 = _elt(flags), torch.float32
+    for t, m, name in ((res, T * d, "res"), (y, T * d, "y"), (gate, _gate_count(flags, T, d), "gate"),
+                       (w_post, d, "w_post"), (w_pre, d, "w_pre"), (r, T * d, "r"), (n, T * d, "n")):
+        _need(t, m, name, el)
+    _need(rstd_post, T, "rstd_post", f32)
+    _need(rstd_pre, T, "rstd_pre", f32)
+    _here(res, y, gate, w_post, w_pre, r, n, rstd_post, rstd_pre)
+    _check(load_library().moe_norm_fwd(_ptr(res), _ptr(y), _ptr(gate), _ptr(w_post), _ptr(w_pre),
+                                       res_scale, eps, T, d, flags, _ptr(r), _ptr(n),
+                                       _ptr(rstd_post), _ptr(rstd_pre), _stream(stream)))
+
+
+@functools.lru_cache(maxsize=256, typed=True)
+def moe_norm_bwd_workspace_size(T, d, flags) -> int:
+    return load_library().moe_norm_bwd_workspace_size(T, d, flags)
+
+
+def moe_norm_bwd(dr, dn, y, r, gate, w_post, w_pre, rstd_post, rstd_pre, res_scale, T, d, flags,
+                 dres, dy, dgate, dw_post, dw_pre, workspace, workspace_bytes, stream=None):
+    el, f32 = _elt(flags), torch.float32
+    ng = _gate_count(flags, T, d)
+    full = flags & MOE_GATE_CHANNEL and flags & MOE_GATE_TOKEN
+    for t, m, name in ((dr, T * d, "dr"), (dn, T * d, "dn"), (y, T * d, "y"), (r, T * d, "r"),
+                       (gate, ng, "gate"), (w_post, d, "w_post"), (w_pre, d, "w_pre"),
+                       (dres, T * d, "dres"), (dy, T * d, "dy")):
+        _need(t, m, name, el)
+    for t, m, name in ((rstd_post, T, "rstd_post"), (rstd_pre, T, "rstd_pre"),
+                       (dw_post, d, "dw_post"), (dw_pre, d, "dw_pre")):
+        _need(t, m, name, f32)
+    _need(dgate, ng, "dgate", el if full else f32)
+    _need_bytes(workspace, workspace_bytes)
+    _here(dr, dn, y, r, gate, w_post, w_pre, rstd_post, rstd_pre, dres, dy, dgate, dw_post, dw_pre,
+          workspace)
+    _check(load_library().moe_norm_bwd(
+        _ptr(dr), _ptr(dn), _ptr(y), _ptr(r), _ptr(gate), _ptr(w_post), _ptr(w_pre),
+        _ptr(rstd_post), _ptr(rstd_pre), res_scale, T, d, flags, _ptr(dres), _ptr(dy), _ptr(dgate),
+        _ptr(dw_post), _ptr(dw_pre), _ptr(workspace), workspace_bytes, _stream(stream)))
+
+
+@functools.lru_cache(maxsize=256, typed=True)
+def moe_grad_norm_workspace_size(n) -> int:
+    return load_library().moe_grad_norm_workspace_size(n)
+
+
+class TensorList:
+    """The host arrays (pointers, element counts, types) that the gradient calls take of a
+    list of contiguous bfloat16 and float32 tensors."""
+
+    def __init__(self, tensors):
+        self.tensors = list(tensors)
+        _here(*self.tensors)
+        n = len(self.tensors)
+        self.n = n
+        self.ptrs = (ctypes.c_void_p * n)(*[_ptr(t) for t in self.tensors])
+        self.sizes = (ctypes.c_int64 * n)(*[t.numel() for t in self.tensors])
+        self.types = (ctypes.c_uint * n)(*[dtype_flag(t) for t in self.tensors])
+
+
+def moe_grad_norm(grads: TensorList, sumsq, norm, workspace, workspace_bytes, stream=None):
+    _need(sumsq, 1, "sumsq", torch.float64)
+    _need(norm, 1, "norm", torch.float32)
+    _need_bytes(workspace, workspace_bytes)
+    _here(sumsq, norm, workspace)
+    _check(load_library().moe_grad_norm(grads.ptrs, grads.sizes, grads.types, grads.n, _ptr(sumsq),
+                                        _ptr(norm), _ptr(workspace), workspace_bytes,
+                                        _stream(stream)))
+
+
+def moe_grad_clip(grads: TensorList, outs, sumsq, max_norm, stream=None):
+    """`outs`: a TensorList of the same sizes and types, or None (in place)."""
+    _need(sumsq, 1, "sumsq", torch.float64)
+    _here(sumsq)
+    if outs is not None:
+        if list(outs.sizes) != list(grads.sizes) or list(outs.types) != list(grads.types):
+            raise ValueError("outs: not the gradients' sizes and types")
+    _check(load_library().moe_grad_clip(grads.ptrs, None if outs is None else outs.ptrs, grads.sizes,
+                                        grads.types, grads.n, _ptr(sumsq), max_norm,
+                                        _stream(stream)))
+
+
+def moe_mx_quantize(src, batch, R, K, flags, codes, scales, stream=None):
+    n = batch * R * K
+    _need(src, n, "src", _elt(flags))
+    _need(codes, n // 2, "codes", torch.uint8)
+    _need(scales, n // 32, "scales", torch.uint8)
+    _here(src, codes, scales)
+    _check(load_library().moe_mx_quantize(_ptr(src), batch, R, K, flags, _ptr(codes), _ptr(scales),
+                                          _stream(stream)))
+
+
+def moe_mx_dequantize(codes, scales, R, K, flags, out, stream=None):
+    _need(codes, R * K // 2, "codes", torch.uint8)
+    _need(scales, R * K // 32, "scales", torch.uint8)
+    _need(out, R * K, "out", _elt(flags))
+    _here(codes, scales, out)
+    _check(load_library().moe_mx_dequantize(_ptr(codes), _ptr(scales), R, K, flags, _ptr(out),
+                                            _stream(stream)))
+
+
+def moe_mx_gemm(x, x_scales, w, w_scales, w3, w3_scales, offsets, rows, T, S, K, N, E, flags, out,
+                stream=None):
+    u8 = torch.uint8
+    if x_scales is None:
+        _need(x, T * K, "x", torch.bfloat16)
+    else:
+        _need(x, T * K // 2, "x", u8)
+        _need(x_scales, T * K // 32, "x_scales", u8)
+    for t, m, name in ((w, E * N * K // 2, "w"), (w_scales, E * N * K // 32, "w_scales"),
+                       (w3, E * N * K // 2, "w3"), (w3_scales, E * N * K // 32, "w3_scales")):
+        _need(t, m, name, u8)
+    _need(offsets, E + 1, "offsets", torch.int32)
+    _need(rows, S, "rows", torch.int32)
+    _need(out, S * N, "out", torch.bfloat16)
+    _here(x, x_scales, w, w_scales, w3, w3_scales, offsets, rows, out)
+    _check(load_library().moe_mx_gemm(_ptr(x), _ptr(x_scales), _ptr(w), _ptr(w_scales), _ptr(w3),
+                                      _ptr(w3_scales), _ptr(offsets), _ptr(rows), T, S, K, N, E,
+                                      flags, _ptr(out), _stream(stream)))
 
 
 def moe_probe_enable(capacity: int):

@@ -1,7 +1,12 @@
 // api.cpp -- the extern "C" entry points of libmoeblaze.so: argument
 // validation (before anything is enqueued), then the internal launchers.
+#include <math.h>
 #include <stdarg.h>
 #include <stdio.h>
+
+#include <algorithm>
+#include <new>
+#include <vector>
 
 #include "../../include/moeblaze.h"
 #include "launch.hpp"
@@ -414,6 +419,290 @@ int moe_route_bwd(const float* d_gates, const float* logits, const int32_t* topk
     return hip_status(fn, moe::route_bwd(d_gates, logits, topk_ids, gates, x, w_gate, T, d, E, k,
                                          flags & MOE_F32, flags & MOE_RENORM,
                                          flags & MOE_ACCUMULATE, dw_gate, dx, workspace, stream));
+}
+
+// ---- norms of a residual block ----
+
+}  // extern "C"
+
+namespace {
+
+// flags and sizes of the norm calls; `gate_kind`: 0 none, 1 [d], 2 [T], 3 [T, d]
+int check_norm(const char* fn, int64_t T, int d, float res_scale, unsigned flags, int* gate_kind) {
+    const unsigned known = MOE_F32 | MOE_NORM_POST | MOE_NORM_PRE | MOE_GATE_CHANNEL | MOE_GATE_TOKEN;
+    if (flags & ~known) return fail(MOE_ERR_INVALID_ARG, "%s: unknown flag bits 0x%x", fn, flags & ~known);
+    if (T < 0) return fail(MOE_ERR_INVALID_ARG, "%s: T = %lld < 0", fn, (long long)T);
+    if (d < 1) return fail(MOE_ERR_INVALID_ARG, "%s: d = %d < 1", fn, d);
+    if (d % 8) return fail(MOE_ERR_UNSUPPORTED, "%s: d = %d is not a multiple of 8", fn, d);
+    if (d > 8192) return fail(MOE_ERR_UNSUPPORTED, "%s: d = %d > 8192", fn, d);
+    if (!isfinite(res_scale)) return fail(MOE_ERR_INVALID_ARG, "%s: res_scale is not finite", fn);
+    *gate_kind = (flags & MOE_GATE_CHANNEL ? 1 : 0) + (flags & MOE_GATE_TOKEN ? 2 : 0);
+    return MOE_OK;
+}
+
+// what a call without a block output may not ask for
+int check_no_block(const char* fn, float res_scale, unsigned flags) {
+    if (flags & (MOE_NORM_POST | MOE_GATE_CHANNEL | MOE_GATE_TOKEN))
+        return fail(MOE_ERR_INVALID_ARG, "%s: a post-norm or a gate without a block output", fn);
+    if (!(flags & MOE_NORM_PRE))
+        return fail(MOE_ERR_INVALID_ARG, "%s: neither a block output nor MOE_NORM_PRE: nothing to do", fn);
+    if (res_scale != 1.0f)
+        return fail(MOE_ERR_INVALID_ARG, "%s: res_scale must be 1 without a block output", fn);
+    return MOE_OK;
+}
+
+// a pointer that a flag asks for, and that must be NULL without it
+#define FLAG_PTR(p, on, why)                                                                   \
+    do {                                                                                       \
+        if (on) REQUIRE_PTR(p);                                                                \
+        else if (p) return fail(MOE_ERR_INVALID_ARG, "%s: %s without %s", fn, #p, why);        \
+    } while (0)
+
+struct Span {
+    uintptr_t lo, hi;
+    bool written;
+    int tensor;   // a gradient and its own output share a number
+};
+
+}  // namespace
+
+extern "C" {
+
+int moe_norm_fwd(const void* res, const void* y, const void* gate, const void* w_post,
+                 const void* w_pre, float res_scale, float eps, int64_t T, int d, unsigned flags,
+                 void* r, void* n, float* rstd_post, float* rstd_pre, hipStream_t stream) {
+    const char* fn = "moe_norm_fwd";
+    int e, kind;
+    if ((e = check_norm(fn, T, d, res_scale, flags, &kind))) return e;
+    if (!(eps > 0.0f) || !isfinite(eps)) return fail(MOE_ERR_INVALID_ARG, "%s: eps must be positive and finite", fn);
+    if (T == 0) return MOE_OK;
+    if (!y && (e = check_no_block(fn, res_scale, flags))) return e;
+    REQUIRE_PTR(res); OPT_PTR(y); OPT_PTR(rstd_post); OPT_PTR(rstd_pre);
+    FLAG_PTR(r, y != nullptr, "a block output");
+    FLAG_PTR(gate, kind, "a gate flag");
+    FLAG_PTR(w_post, flags & MOE_NORM_POST, "MOE_NORM_POST");
+    FLAG_PTR(w_pre, flags & MOE_NORM_PRE, "MOE_NORM_PRE");
+    FLAG_PTR(n, flags & MOE_NORM_PRE, "MOE_NORM_PRE");
+    if (r && r == n) return fail(MOE_ERR_INVALID_ARG, "%s: r and n are the same", fn);
+    moe::NormArgs a{};
+    a.res = res; a.y = y; a.gate = gate; a.w_post = w_post; a.w_pre = w_pre; a.r = r; a.n = n;
+    a.rstd_post = rstd_post; a.rstd_pre = rstd_pre; a.res_scale = res_scale; a.eps = eps;
+    a.T = T; a.d = d; a.gate_kind = kind; a.f32 = flags & MOE_F32;
+    moe::probe::begin(stream);
+    return hip_status(fn, moe::norm_fwd(a, stream));
+}
+
+size_t moe_norm_bwd_workspace_size(int64_t T, int d, unsigned flags) {
+    if (T <= 0 || d < 1 || d > 8192) return 0;
+    return moe::norm_bwd_workspace(T, d, flags & MOE_F32);
+}
+
+int moe_norm_bwd(const void* dr, const void* dn, const void* y, const void* r, const void* gate,
+                 const void* w_post, const void* w_pre, const float* rstd_post,
+                 const float* rstd_pre, float res_scale, int64_t T, int d, unsigned flags,
+                 void* dres, void* dy, void* dgate, float* dw_post, float* dw_pre, void* workspace,
+                 size_t workspace_bytes, hipStream_t stream) {
+    const char* fn = "moe_norm_bwd";
+    int e, kind;
+    if ((e = check_norm(fn, T, d, res_scale, flags, &kind))) return e;
+    const bool post = flags & MOE_NORM_POST, pre = flags & MOE_NORM_PRE;
+    FLAG_PTR(w_post, post, "MOE_NORM_POST"); FLAG_PTR(dw_post, post, "MOE_NORM_POST");
+    FLAG_PTR(w_pre, pre, "MOE_NORM_PRE"); FLAG_PTR(dw_pre, pre, "MOE_NORM_PRE");
+    FLAG_PTR(dgate, kind, "a gate flag");
+    if (T > 0) {
+        if (!dy && (e = check_no_block(fn, res_scale, flags))) return e;
+        if (!dr && !pre) return fail(MOE_ERR_INVALID_ARG, "%s: neither dr nor MOE_NORM_PRE: no gradient comes in", fn);
+        REQUIRE_PTR(dres); OPT_PTR(dr); OPT_PTR(dy); OPT_PTR(y); OPT_PTR(r);
+        FLAG_PTR(gate, kind, "a gate flag");
+        FLAG_PTR(dn, pre, "MOE_NORM_PRE");
+        if (pre) { REQUIRE_PTR(r); REQUIRE_PTR(rstd_pre); }
+        if (post) REQUIRE_PTR(rstd_post);
+        if (post || kind) REQUIRE_PTR(y);
+        if (dres == dy) return fail(MOE_ERR_INVALID_ARG, "%s: dres and dy are the same", fn);
+        const size_t need = moe::norm_bwd_workspace(T, d, flags & MOE_F32);
+        if (!workspace || workspace_bytes < need)
+            return fail(MOE_ERR_WORKSPACE, "%s: workspace %zu bytes < %zu needed", fn, workspace_bytes, need);
+        REQUIRE_PTR(workspace);
+    }
+    moe::NormArgs a{};
+    a.dr = dr; a.dn = dn; a.y = y; a.r = const_cast<void*>(r); a.gate = gate; a.w_post = w_post;
+    a.w_pre = w_pre; a.rstd_post = const_cast<float*>(rstd_post);
+    a.rstd_pre = const_cast<float*>(rstd_pre); a.res_scale = res_scale; a.T = T; a.d = d;
+    a.gate_kind = kind; a.f32 = flags & MOE_F32; a.dres = dres; a.dy = dy; a.dgate = dgate;
+    a.dw_post = dw_post; a.dw_pre = dw_pre; a.part = static_cast<float*>(workspace);
+    moe::probe::begin(stream);
+    return hip_status(fn, moe::norm_bwd(a, stream));
+}
+
+// ---- gradient norm and clipping ----
+
+}  // extern "C"
+
+namespace {
+
+int check_grads(const char* fn, const void* const* grads, const int64_t* sizes, const unsigned* types,
+                int n) {
+    if (n < 0) return fail(MOE_ERR_INVALID_ARG, "%s: n = %d < 0", fn, n);
+    if (n > (1 << 20)) return fail(MOE_ERR_UNSUPPORTED, "%s: n = %d > 2^20 tensors", fn, n);
+    if (n && (!grads || !sizes || !types)) return fail(MOE_ERR_INVALID_ARG, "%s: a NULL list", fn);
+    for (int i = 0; i < n; ++i) {
+        if (sizes[i] < 0) return fail(MOE_ERR_INVALID_ARG, "%s: sizes[%d] = %lld < 0", fn, i, (long long)sizes[i]);
+        if (sizes[i] > (int64_t(1) << 44)) return fail(MOE_ERR_UNSUPPORTED, "%s: sizes[%d] > 2^44", fn, i);
+        if (types[i] != MOE_BF16 && types[i] != MOE_F32)
+            return fail(MOE_ERR_INVALID_ARG, "%s: types[%d] = 0x%x is neither MOE_BF16 nor MOE_F32", fn, i, types[i]);
+        if (sizes[i] && !grads[i]) return fail(MOE_ERR_INVALID_ARG, "%s: grads[%d] is NULL", fn, i);
+        if (sizes[i] && reinterpret_cast<uintptr_t>(grads[i]) % (types[i] == MOE_F32 ? 4 : 2))
+            return fail(MOE_ERR_INVALID_ARG, "%s: grads[%d] is not aligned to its elements", fn, i);
+    }
+    return MOE_OK;
+}
+
+// Among the tensors that a clip reads and writes, no written one may share memory with
+// another. O(n log n) on the host.
+int check_overlap(const char* fn, const void* const* grads, void* const* outs, const int64_t* sizes,
+                  const unsigned* types, int n) {
+    std::vector<Span> v;
+    v.reserve(2 * (size_t)n);
+    for (int i = 0; i < n; ++i) {
+        if (sizes[i] == 0) continue;
+        const uintptr_t bytes = (uintptr_t)sizes[i] * (types[i] == MOE_F32 ? 4 : 2);
+        const uintptr_t g = reinterpret_cast<uintptr_t>(grads[i]);
+        const uintptr_t o = outs ? reinterpret_cast<uintptr_t>(outs[i]) : g;
+        if (o == g) {
+            v.push_back({g, g + bytes, true, i});
+        } else {
+            v.push_back({g, g + bytes, false, i});
+            v.push_back({o, o + bytes, true, i});
+        }
+    }
+    std::sort(v.begin(), v.end(), [](const Span& a, const Span& b) { return a.lo < b.lo; });
+    // the furthest end so far, of all spans and of the written ones
+    uintptr_t end = 0, wend = 0;
+    int who = 0, wwho = 0;
+    for (const Span& s : v) {
+        if (s.written && s.lo < end)
+            return fail(MOE_ERR_INVALID_ARG, "%s: tensors %d and %d overlap, and one of them is written", fn, who, s.tensor);
+        if (s.lo < wend)
+            return fail(MOE_ERR_INVALID_ARG, "%s: tensors %d and %d overlap, and one of them is written", fn, wwho, s.tensor);
+        if (s.hi > end) { end = s.hi; who = s.tensor; }
+        if (s.written && s.hi > wend) { wend = s.hi; wwho = s.tensor; }
+    }
+    return MOE_OK;
+}
+
+}  // namespace
+
+extern "C" {
+
+size_t moe_grad_norm_workspace_size(int n) { return n < 1 ? 0 : moe::grad_norm_workspace(n); }
+
+int moe_grad_norm(const void* const* grads, const int64_t* sizes, const unsigned* types, int n,
+                  double* sumsq, float* norm, void* workspace, size_t workspace_bytes,
+                  hipStream_t stream) {
+    const char* fn = "moe_grad_norm";
+    int e;
+    if ((e = check_grads(fn, grads, sizes, types, n))) return e;
+    if (!sumsq || reinterpret_cast<uintptr_t>(sumsq) % 8) return fail(MOE_ERR_INVALID_ARG, "%s: sumsq is NULL or not aligned", fn);
+    if (!norm || reinterpret_cast<uintptr_t>(norm) % 4) return fail(MOE_ERR_INVALID_ARG, "%s: norm is NULL or not aligned", fn);
+    const size_t need = moe_grad_norm_workspace_size(n);
+    if (need && (!workspace || workspace_bytes < need))
+        return fail(MOE_ERR_WORKSPACE, "%s: workspace %zu bytes < %zu needed", fn, workspace_bytes, need);
+    OPT_PTR(workspace);
+    moe::probe::begin(stream);
+    return hip_status(fn, moe::grad_norm(grads, sizes, types, n, sumsq, norm, workspace, stream));
+}
+
+int moe_grad_clip(const void* const* grads, void* const* outs, const int64_t* sizes,
+                  const unsigned* types, int n, const double* sumsq, double max_norm,
+                  hipStream_t stream) {
+    const char* fn = "moe_grad_clip";
+    int e;
+    if ((e = check_grads(fn, grads, sizes, types, n))) return e;
+    if (!(max_norm >= 0.0)) return fail(MOE_ERR_INVALID_ARG, "%s: max_norm must be zero or more", fn);
+    if (!sumsq || reinterpret_cast<uintptr_t>(sumsq) % 8) return fail(MOE_ERR_INVALID_ARG, "%s: sumsq is NULL or not aligned", fn);
+    for (int i = 0; outs && i < n; ++i)
+        if (sizes[i] && (!outs[i] || reinterpret_cast<uintptr_t>(outs[i]) % (types[i] == MOE_F32 ? 4 : 2)))
+            return fail(MOE_ERR_INVALID_ARG, "%s: outs[%d] is NULL or not aligned to its elements", fn, i);
+    try {
+        if ((e = check_overlap(fn, grads, outs, sizes, types, n))) return e;
+    } catch (const std::bad_alloc&) {
+        return fail(MOE_ERR_INVALID_ARG, "%s: no host memory for %d tensors", fn, n);
+    }
+    moe::probe::begin(stream);
+    return hip_status(fn, moe::grad_clip(grads, outs ? outs : const_cast<void* const*>(grads), sizes,
+                                         types, n, sumsq, max_norm, stream));
+}
+
+// ---- microscaled 4-bit values and the products over them ----
+
+int moe_mx_quantize(const void* src, int64_t batch, int64_t R, int K, unsigned flags, void* codes,
+                    void* scales, hipStream_t stream) {
+    const char* fn = "moe_mx_quantize";
+    const unsigned known = MOE_F32 | MOE_TRANSPOSED;
+    if (flags & ~known) return fail(MOE_ERR_INVALID_ARG, "%s: unknown flag bits 0x%x", fn, flags & ~known);
+    if (batch < 0 || R < 0) return fail(MOE_ERR_INVALID_ARG, "%s: batch = %lld, R = %lld", fn, (long long)batch, (long long)R);
+    if (K < 1) return fail(MOE_ERR_INVALID_ARG, "%s: K = %d < 1", fn, K);
+    if (K % 32) return fail(MOE_ERR_UNSUPPORTED, "%s: K = %d is not a multiple of 32", fn, K);
+    if ((double)batch * (double)R * K >= 68719476736.0)
+        return fail(MOE_ERR_UNSUPPORTED, "%s: 2^36 values or more", fn);
+    if (flags & MOE_TRANSPOSED) {
+        if (R % 2) return fail(MOE_ERR_UNSUPPORTED, "%s: R = %lld is odd (MOE_TRANSPOSED)", fn, (long long)R);
+        if (batch > 65535) return fail(MOE_ERR_UNSUPPORTED, "%s: batch = %lld > 65535 (MOE_TRANSPOSED)", fn, (long long)batch);
+        if (K > 65535 * 256) return fail(MOE_ERR_UNSUPPORTED, "%s: K = %d > 65535 * 256 (MOE_TRANSPOSED)", fn, K);
+    }
+    if (batch == 0 || R == 0) return MOE_OK;
+    REQUIRE_PTR(src); REQUIRE_PTR(codes); REQUIRE_PTR(scales);
+    moe::probe::begin(stream);
+    return hip_status(fn, moe::mx_quantize(src, batch, R, K, flags & MOE_F32, flags & MOE_TRANSPOSED,
+                                           codes, scales, stream));
+}
+
+int moe_mx_dequantize(const void* codes, const void* scales, int64_t R, int K, unsigned flags,
+                      void* out, hipStream_t stream) {
+    const char* fn = "moe_mx_dequantize";
+    if (flags & ~MOE_F32) return fail(MOE_ERR_INVALID_ARG, "%s: unknown flag bits 0x%x", fn, flags & ~MOE_F32);
+    if (R < 0) return fail(MOE_ERR_INVALID_ARG, "%s: R = %lld < 0", fn, (long long)R);
+    if (K < 1) return fail(MOE_ERR_INVALID_ARG, "%s: K = %d < 1", fn, K);
+    if (K % 32) return fail(MOE_ERR_UNSUPPORTED, "%s: K = %d is not a multiple of 32", fn, K);
+    if ((double)R * K >= 68719476736.0) return fail(MOE_ERR_UNSUPPORTED, "%s: 2^36 values or more", fn);
+    if (R == 0) return MOE_OK;
+    REQUIRE_PTR(codes); REQUIRE_PTR(scales); REQUIRE_PTR(out);
+    moe::probe::begin(stream);
+    return hip_status(fn, moe::mx_dequantize(codes, scales, R * K, flags & MOE_F32, out, stream));
+}
+
+int moe_mx_gemm(const void* x, const void* x_scales, const void* w, const void* w_scales,
+                const void* w3, const void* w3_scales, const int32_t* offsets, const int32_t* rows,
+                int64_t T, int64_t S, int K, int N, int E, unsigned flags, void* out,
+                hipStream_t stream) {
+    const char* fn = "moe_mx_gemm";
+    const unsigned known = MOE_F32 | ACT_FLAGS | MOE_GATED;
+    int r;
+    if (flags & ~known) return fail(MOE_ERR_INVALID_ARG, "%s: unknown flag bits 0x%x", fn, flags & ~known);
+    if (flags & MOE_F32) return fail(MOE_ERR_UNSUPPORTED, "%s: bfloat16 only", fn);
+    const unsigned act = flags & (ACT_FLAGS | MOE_GATED);
+    if (act & (act - 1)) return fail(MOE_ERR_INVALID_ARG, "%s: at most one of MOE_GATED, MOE_ACT_SILU, MOE_ACT_RELU", fn);
+    if (T < 0 || S < 0) return fail(MOE_ERR_INVALID_ARG, "%s: T = %lld, S = %lld", fn, (long long)T, (long long)S);
+    if (E < 1) return fail(MOE_ERR_INVALID_ARG, "%s: E = %d < 1", fn, E);
+    if (E > 256) return fail(MOE_ERR_UNSUPPORTED, "%s: E = %d > 256", fn, E);
+    if ((r = check_dim(fn, "K", K)) || (r = check_dim(fn, "N", N))) return r;
+    if (S >= (int64_t(1) << 31) || T >= (int64_t(1) << 31))
+        return fail(MOE_ERR_UNSUPPORTED, "%s: T = %lld, S = %lld do not fit int32", fn, (long long)T, (long long)S);
+    if (!rows && S != T) return fail(MOE_ERR_INVALID_ARG, "%s: rows is NULL and T = %lld is not S = %lld", fn, (long long)T, (long long)S);
+    if (S > 0 && T == 0) return fail(MOE_ERR_INVALID_ARG, "%s: T = 0 with S = %lld slots", fn, (long long)S);
+    if (S == 0) return MOE_OK;
+    REQUIRE_PTR(x); REQUIRE_PTR(w); REQUIRE_PTR(w_scales); REQUIRE_PTR(offsets); REQUIRE_PTR(out);
+    OPT_PTR(x_scales); OPT_PTR(rows);
+    FLAG_PTR(w3, flags & MOE_GATED, "MOE_GATED");
+    FLAG_PTR(w3_scales, flags & MOE_GATED, "MOE_GATED");
+    moe::MxArgs a{};
+    a.x = x; a.xs = static_cast<const uint8_t*>(x_scales);
+    a.w = static_cast<const uint8_t*>(w); a.ws = static_cast<const uint8_t*>(w_scales);
+    a.w3 = static_cast<const uint8_t*>(w3); a.ws3 = static_cast<const uint8_t*>(w3_scales);
+    a.offsets = offsets; a.rows = rows; a.T = T; a.S = S; a.N = N; a.K = K; a.E = E;
+    a.act = act_of(flags); a.out = out;
+    moe::probe::begin(stream);
+    return hip_status(fn, moe::mx_gemm(a, stream));
 }
 
 }  // extern "C"

@@ -88,4 +88,46 @@ hipError_t small_dact(const FfnArgs& a, SmallTile v, const float* gs, void* HG, 
 hipError_t small_dx(const FfnArgs& a, SmallTile v, int c0, int nc, int64_t ldo, void* out, bool scatter,
                     hipStream_t st);
 
+// ---- norms of a residual block (norm.hip) ----
+struct NormArgs {
+    const void *res, *y, *gate, *w_post, *w_pre;   // w_post / w_pre: null where that norm is off
+    void *r, *n;
+    float *rstd_post, *rstd_pre;
+    float res_scale, eps;
+    int64_t T;
+    int d, gate_kind;   // 0 none, 1 [d], 2 [T], 3 [T, d]
+    bool f32;
+    const void *dr, *dn;
+    void *dres, *dy, *dgate;
+    float *dw_post, *dw_pre, *part;
+};
+hipError_t norm_fwd(const NormArgs& a, hipStream_t st);
+size_t norm_bwd_workspace(int64_t T, int d, bool f32);
+hipError_t norm_bwd(const NormArgs& a, hipStream_t st);
+
+// ---- gradient norm and clipping (grads.hip) ----
+size_t grad_norm_workspace(int n);
+hipError_t grad_norm(const void* const* g, const int64_t* sizes, const unsigned* types, int n,
+                     double* sumsq, float* norm, void* ws, hipStream_t st);
+hipError_t grad_clip(const void* const* g, void* const* out, const int64_t* sizes,
+                     const unsigned* types, int n, const double* sumsq, double max_norm,
+                     hipStream_t st);
+
+// ---- microscaled 4-bit values (mx.hip) ----
+hipError_t mx_quantize(const void* src, int64_t batch, int64_t R, int K, bool f32, bool transposed,
+                       void* codes, void* scales, hipStream_t st);
+hipError_t mx_dequantize(const void* codes, const void* scales, int64_t n, bool f32, void* out,
+                         hipStream_t st);
+
+// ---- grouped products over microscaled weights (mx_gemm.hip) ----
+struct MxArgs {
+    const void* x; const uint8_t* xs;              // rows: bfloat16, or codes and their scales
+    const uint8_t *w, *ws, *w3, *ws3;              // w3: null unless gated
+    const int32_t *offsets, *rows;                 // rows: null where slot s is row s
+    int64_t T, S;
+    int N, K, E, act;                              // act: 0 none or gated, 1 SiLU, 2 ReLU
+    void* out;
+};
+hipError_t mx_gemm(const MxArgs& a, hipStream_t st);
+
 }  // namespace moe

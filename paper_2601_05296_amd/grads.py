@@ -1,0 +1,50 @@
+"""The global norm of gradients, and clipping by it, over any list of tensors: the
+layer's own gradients are float32, a model's others may be bfloat16."""
+from __future__ import annotations
+
+import torch
+
+from . import binding as B
+from .layer import _on
+
+
+def _list(grads):
+    """The tensors of a list, tuple or dict (as layer.backward returns), without None."""
+    return [g for g in (grads.values() if isinstance(grads, dict) else grads) if g is not None]
+
+
+def _norm(tl, dev):
+    norm = torch.empty((), dtype=torch.float32, device=dev)
+    sumsq = torch.empty((), dtype=torch.float64, device=dev)
+    wsb = B.moe_grad_norm_workspace_size(tl.n)
+    ws = torch.empty(max(wsb, 16), dtype=torch.uint8, device=dev)
+    B.moe_grad_norm(tl, sumsq, norm, ws, wsb, None)
+    return norm, sumsq
+
+
+def norm(grads, stream=None):
+    """(norm, sumsq): the 2-norm over all elements of all tensors, float32, and its square,
+    float64, both on the GPU. Where a model's gradients are spread over several devices the
+    devices' sumsq add up."""
+    with _on(stream):
+        tl = B.TensorList(_list(grads))
+        return _norm(tl, tl.tensors[0].device if tl.n else torch.device("cuda", torch.cuda.current_device()))
+
+
+def clip(grads, max_norm: float, out=None, sumsq=None, stream=None):
+    """Scale the gradients by min(1, max_norm / (norm + 1e-6)), in place or into ``out``
+    (tensors of the same sizes and types, in the same order). ``sumsq``: the square of the
+    norm to go by (a float64 GPU tensor: the sum over several devices'), None: these
+    tensors' own. Returns the norm, on the GPU; nothing waits for the host."""
+    with _on(stream):
+        tl = B.TensorList(_list(grads))
+        outs = None if out is None else B.TensorList(_list(out))
+        if outs is not None and outs.n != tl.n:
+            raise ValueError("out: %d tensors for %d gradients" % (outs.n, tl.n))
+        dev = tl.tensors[0].device if tl.n else torch.device("cuda", torch.cuda.current_device())
+        if sumsq is None:
+            total, sumsq = _norm(tl, dev)
+        else:
+            total = sumsq.sqrt().float()
+        B.moe_grad_clip(tl, outs, sumsq, max_norm, None)
+    return total
