@@ -169,10 +169,10 @@ def _run(dev, ref, tol, spare=0):
     assert (got[ref.shape[0]:] == 77.0).all()
 
 
-# rows of each expert, chosen so that the mean picks each core: streams of 16 and 32 rows,
+# rows of each expert, chosen so that the mean picks each core: streams of 4, 16 and 32 rows,
 # tiles of 64, 128 and 256
 LOADS = {
-    "one": [0, 0, 1, 0], "few": [3, 0, 17, 1, 0, 16, 0], "some": [40, 2, 0, 33, 16],
+    "one": [0, 0, 1, 0], "same": [0, 7, 0, 0, 0, 0, 0, 0], "few": [3, 0, 17, 1, 0, 16, 0], "some": [40, 2, 0, 33, 16],
     "tile64": [64, 1, 0, 130, 33], "tile128": [129, 128, 3, 0, 200], "tile256": [256, 300, 0, 1, 700, 255],
 }
 
@@ -194,7 +194,7 @@ def test_product_loads_reach_every_core():
     for load, counts in LOADS.items():
         dev, *_ = _case(counts, 50, 128, 64, "none", False, True)
         names[load] = launched(lambda: mx.product(**dev))
-    assert [names[n] for n in LOADS] == [["mx_stream"]] * 3 + [["mx_tile"]] * 3
+    assert [names[n] for n in LOADS] == [["mx_stream"]] * 4 + [["mx_tile"]] * 3
 
 
 @pytest.mark.parametrize("act", ["silu", "relu"])
@@ -210,6 +210,22 @@ def test_product_widths(K, N, x4):
     for counts in ([5, 0, 9], [70, 31]):
         print(K, N, x4, counts, flush=True)
         _run(*_case(counts, 33, K, N, "swiglu", x4, True, seed=1))
+
+
+@pytest.mark.parametrize("K", [4096, 4160, 8256, 14336])
+@pytest.mark.parametrize("x4", [False, True])
+def test_product_deep(K, x4):
+    """Long sums on few workgroups, the scales reloaded on the way, rows not whole slices."""
+    for counts in ([1, 0, 1], [11, 0, 2], [25, 9], [90, 41], [300]):
+        print(K, x4, counts, flush=True)
+        _run(*_case(counts, 27, K, 64, "none", x4, len(counts) > 1, seed=K))
+
+
+@pytest.mark.parametrize("x4", [False, True])
+def test_product_wide(x4):
+    """More workgroups than CUs for a row or two, and wide enough for every column split."""
+    for counts in ([1, 0, 2, 0, 1, 0], [20, 30]):
+        _run(*_case(counts, 5, 192, 14336, "swiglu", x4, True, seed=7))
 
 
 @pytest.mark.parametrize("x4", [False, True])
