@@ -299,15 +299,12 @@ mx_stream(const Args a) {
 // of chunk c, while slices of chunk c - 1 may still be read. (One 16-bit copy a lane for
 // each two blocks, every lane in a row of its own, cost 14% with bfloat16 rows and 25% with
 // 4-bit ones.) Where a row has an odd number of pairs of blocks, odd rows start in the
-// middle of a dword: their chunks begin two bytes early, and `odd` is added to the pair.
+// middle of a dword: their chunks begin two bytes early. (The last dword of all may end two
+// bytes behind the last scale of x; those bytes are not used.)
 
-// 4-byte and 2-byte global -> LDS copies: lane l writes the dword at lds_off + 4 l
+// 4-byte global -> LDS copy: lane l writes the dword at lds_off + 4 l
 __device__ __forceinline__ void dma4(const void* g, uint32_t lds_off) {
     asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dword %0, off"
-                 ::"v"(g), "s"(lds_off) : "memory", "m0");
-}
-__device__ __forceinline__ void dma2(const void* g, uint32_t lds_off) {
-    asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_ushort %0, off"
                  ::"v"(g), "s"(lds_off) : "memory", "m0");
 }
 
@@ -330,9 +327,9 @@ struct TCfg {
     static constexpr int STAGE = X_BYTES + W_BYTES, RING = NST * STAGE;
     static constexpr int LDS = RING + 3 * S_BYTES;
     static constexpr int PER = NCX + NCW + NCP;
-    static_assert(SROWS % (16 * NW) == 0, "scale rows");
+    static_assert(SROWS % (16 * NW) == 0 && NST <= SPC + 1, "scale rows, buffers");
     static_assert(X_BYTES % (1024 * NW) == 0 && W_BYTES % (1024 * NW) == 0 && NCX >= 1 && NCW >= 1, "copies");
-    static_assert(FM >= 1 && FN >= 1 && LDS <= 160 * 1024 && PER * (NST - 2) < 64, "tile");
+    static_assert(FM >= 1 && FN >= 1 && LDS <= 160 * 1024 && PER * (NST - 1) < 64, "tile");
 };
 
 // 16-byte chunk c of row r in an LDS tile of ROW-byte rows: 128 / ROW rows share a line of
@@ -369,8 +366,9 @@ mx_tile(const Args a) {
     using PX = Place<C::XROW>;
     using PW = Place<C::WROW>;
     // this lane's sources, one for each copy
-    const uint8_t *px[C::NCX], *pw[C::NCW], *ps[C::NCS];
-    int smax[C::NCS];             // last dword of the scale row that this lane copies of
+    const uint8_t *px[C::NCX], *pw[C::NCW], *ps;   // ps + pd[i]: scale row of copy i, from its dword on
+    int64_t pd[C::NCS];
+    int leads = 0;                // bit i: the scale row of this lane's copy i starts in the middle of a dword
     int cx[C::NCX], cw[C::NCW];   // chunk inside the slice
 #pragma unroll
     for (int i = 0; i < C::NCX; ++i) {
@@ -396,43 +394,37 @@ mx_tile(const Args a) {
         if (r < C::NB * C::BN) p = a.ws[C::NB == 2 ? r / C::BN : 0] + column(r) * nkb;
         else p = a.xs + x_row(a, t.off + t.m0 + min(r - C::NB * C::BN, t.mrows - 1)) * nkb;
         const int lead = (int)(reinterpret_cast<uintptr_t>(p) & 2);
-        ps[i] = p - lead;
-        smax[i] = (nkb + lead - 1) & ~3;
+        if (i == 0) ps = p - lead;
+        pd[i] = p - lead - ps;
+        leads |= (lead >> 1) << i;
     }
-    const uint8_t* const xs_end = C::X4 ? a.xs + a.T * nkb : nullptr;
-    const uint32_t base = lds_offset(lds);
-    // all of this wave's copies of slice s; with 4-bit rows the last slice may be half a slice
-    const uint32_t sbase = base + C::RING;
-    // copy i of this wave's of scale chunk c (past the row: its last dword again)
+    const uint32_t base = lds_offset(lds), sbase = base + C::RING;
+    // copy i of this wave's of scale chunk c (past the row: its last dword again); dword d of
+    // row r lies in place d ^ (r / 8) % 4 of the row's four
     auto issue_scales = [&](int i, int c, int buf) __attribute__((always_inline)) {
+        const uint8_t* p = ps;
 #pragma unroll
-        for (int q = 0; q < C::NCS; ++q) {
-            if (q != i) continue;
-            const uint8_t* p = ps[q] + min(c * 16 + (lane & 3) * 4, smax[q]);
-            const uint32_t dst = sbase + buf * C::S_BYTES + (wv * C::NCS + q) * 256;
-            // an odd number of pairs in all of x's rows: the last dword is half outside
-            if (C::X4 && p + 4 == xs_end + 2) dma2(p, dst);
-            else dma4(p, dst);
-        }
+        for (int q = 1; q < C::NCS; ++q) p += i == q ? pd[q] : 0;   // (a select of array elements goes to memory)
+        const int d = (lane ^ ((wv * C::NCS + i) * 2 + (lane >> 5))) & 3;
+        dma4(p + min(c * 16 + d * 4, (nkb + (leads >> i & 1) * 2 - 1) & ~3),
+             sbase + buf * C::S_BYTES + (wv * C::NCS + i) * 256);
     };
     int sbuf = 1;   // buffer of the chunk after the one that the slices being issued are in
-    auto issue = [&](int s, uint32_t dst) __attribute__((always_inline)) {
-#pragma unroll
-        for (int u = 0; u < C::NCP; ++u)
+    // copy u of this wave's C::PER of slice s, slices in order. With 4-bit rows the last slice
+    // may be half a slice: its second half, which is not used, comes from the first.
+    auto issue = [&](int s, uint32_t dst, int u) __attribute__((always_inline)) {
+        const int cut = C::KP == 2 && s * 4 + 4 > nkb ? 2 : 8;
+        if (u < C::NCP) {
             issue_scales((s % C::SPC * C::NCP + u) * C::NCS / (C::SPC * C::NCP), s / C::SPC + 1, sbuf);
-        if ((s + 1) % C::SPC == 0) sbuf = sbuf == 2 ? 0 : sbuf + 1;
-        const bool cut = C::KP == 2 && s * 4 + 4 > nkb;
-#pragma unroll
-        for (int i = 0; i < C::NCX; ++i) {
-            const void* p = px[i] + (int64_t)s * C::XROW;
-            if (cut && cx[i] >= 2) p = &g_zero16;
-            dma16(p, dst + (wv + i * C::NW) * 1024);
-        }
-#pragma unroll
-        for (int i = 0; i < C::NCW; ++i) {
-            const void* p = pw[i] + (int64_t)s * C::WROW;
-            if (cut && cw[i] >= 2) p = &g_zero16;
-            dma16(p, dst + C::X_BYTES + (wv + i * C::NW) * 1024);
+            if (u == C::NCP - 1 && (s + 1) % C::SPC == 0) sbuf = sbuf == 2 ? 0 : sbuf + 1;
+        } else if (u < C::NCP + C::NCX) {
+            const int i = u - C::NCP;
+            dma16(px[i] - (cx[i] >= cut ? 32 : 0), dst + (wv + i * C::NW) * 1024);
+            px[i] += C::XROW;
+        } else {
+            const int i = u - C::NCP - C::NCX;
+            dma16(pw[i] - (cw[i] >= cut ? 32 : 0), dst + C::X_BYTES + (wv + i * C::NW) * 1024);
+            pw[i] += C::WROW;
         }
     };
     f32x16 acc[C::NB][C::FM][C::FN];
@@ -448,90 +440,154 @@ mx_tile(const Args a) {
     __builtin_amdgcn_s_waitcnt(0x0F70);    // vmcnt(0): only copies are outstanding from here on
 #pragma unroll
     for (int i = 0; i < C::NCS; ++i) issue_scales(i, 0, 0);
-    for (int s = 0; s < C::NST - 1 && s < nk; ++s) issue(s, base + s * C::STAGE);
-    const int h = lane >> 5, l32 = lane & 31;
-    // 1 for the fragment rows whose scales start in the middle of a dword (e N is even)
-    int wodd[C::FN], xodd[C::X4 ? C::FM : 1];
+    for (int s = 0; s < C::NST - 1 && s < nk; ++s)
 #pragma unroll
-    for (int j = 0; j < C::FN; ++j)
-        wodd[j] = half_pair ? min(t.n0 + wn * C::WTN + j * 32 + l32, a.N - 1) & 1 : 0;
+        for (int u = 0; u < C::PER; ++u) issue(s, base + s * C::STAGE, u);
+    const int h = lane >> 5, l32 = lane & 31;
+    // whether the scales of x's fragment rows start in the middle of a dword
+    bool odd[C::X4 ? C::FM : 1] = {};
     if constexpr (C::X4)
 #pragma unroll
         for (int i = 0; i < C::FM; ++i)
-            xodd[i] = half_pair ? (int)(x_row(a, t.off + t.m0 + min(wm * C::WTM + i * 32 + l32, t.mrows - 1)) & 1) : 0;
-    int rbuf = 0;   // buffer of the chunk that slice s is in
-    int cur = 0, nxt = C::NST - 1;
-    for (int s = 0; s < nk; ++s) {
-        if (s + C::NST - 2 < nk) wait_vmcnt<C::PER * (C::NST - 2)>();
+            odd[i] = half_pair && (x_row(a, t.off + t.m0 + min(wm * C::WTM + i * 32 + l32, t.mrows - 1)) & 1);
+    int rbuf = 0;      // buffer of the scale chunk that the slice being read is in
+    int cur = 0;       // ring position of the slice being read
+    // LDS place of the scale of block h of pair s KP + k, for a row l32 of 32 whose first is
+    // row 0 (others: 16 bytes a row further on); odd: of a row that starts in mid-dword, whose
+    // last pair lies in the next chunk
+    auto scale_at = [&](int s, int k, int odd) __attribute__((always_inline)) {
+        const int q = s % C::SPC * C::KP + k + odd;
+        const int b = q < 8 ? rbuf : rbuf == 2 ? 0 : rbuf + 1;
+        return C::RING + b * C::S_BYTES + l32 * 16 + (((q & 7) >> 1 ^ ((l32 >> 3) & 3)) << 2) + (q & 1) * 2 + h;
+    };
+    auto byte = [&](int at) __attribute__((always_inline)) {
+        return (uint32_t)*reinterpret_cast<const uint8_t*>(lds + at);
+    };
+    constexpr int NW = C::NB * C::FN, NM = NW * C::FM;   // weight fragments, matrix instructions a step
+    // weight fragment f = b FN + j of pair k; columns of even number (e N and the tile's first
+    // are) start on a dword
+    auto read_w = [&](int s, int k, int f, uint4& w, uint32_t& sw) __attribute__((always_inline)) {
+        const int n = f / C::FN * C::BN + f % C::FN * 32;
+        w = ld16(lds + cur * C::STAGE + C::X_BYTES + PW::byte(wn * C::WTN + l32, 2 * k + h) + n * C::WROW);
+        sw = byte(scale_at(s, k, half_pair ? l32 & 1 : 0) + wn * C::WTN * 16 + n * 16);
+    };
+    auto read_x = [&](int c, int i) __attribute__((always_inline)) {
+        return ld16(lds + cur * C::STAGE + PX::byte(wm * C::WTM + l32, c) + i * 32 * C::XROW);
+    };
+    // A step is NM matrix instructions, each followed by its share of `n` other actions: the
+    // fragment reads of the next step and the copies of a later slice. Both run beside the
+    // matrix instructions then (with all of a slice's copies issued behind its barrier, every
+    // wave at once, the matrix cores waited for some 400 of 2500 cycles a slice).
+    auto step = [&](auto&& mma, int n, auto&& act) __attribute__((always_inline)) {
+#pragma unroll
+        for (int t = 0; t < NM; ++t) {
+            mma(t / (C::FM * C::FN), t / C::FN % C::FM, t % C::FN);
+#pragma unroll
+            for (int u = t * n / NM; u < (t + 1) * n / NM; ++u) act(u);
+            __builtin_amdgcn_sched_barrier(0);
+        }
+    };
+    // between the last fragment reads of slice s and their use: every wave has read slice s,
+    // whose place later copies take, and slice s + 1 is there for all
+    auto next = [&](int s, auto MORE) __attribute__((always_inline)) {
+        if constexpr (decltype(MORE)::value) wait_vmcnt<C::PER * (C::NST - 2)>();
         else wait_vmcnt<0>();
-        lds_barrier();   // slice s is there for all waves, and slice s - 1 has been read by all
-        if (s + C::NST - 1 < nk) issue(s + C::NST - 1, base + nxt * C::STAGE);
-        const char* X = lds + cur * C::STAGE;
-        const char* Wt = X + C::X_BYTES;
-        // the scale byte of this lane's block of pair s KP + k, row r; past K, where the codes
-        // are zeros and LDS may hold the next row's scales (a NaN's), that of 1.0
-        auto scale = [&](int r, int k, int odd) __attribute__((always_inline)) {
-            if (C::KP == 2 && k == 1 && s * 4 + 4 > nkb) return 127u;
-            const int q = s % C::SPC * C::KP + k + odd;       // pair inside the chunk; 8: in the next
-            const int b = q < 8 ? rbuf : rbuf == 2 ? 0 : rbuf + 1;
-            return (uint32_t)*reinterpret_cast<const uint8_t*>(lds + C::RING + b * C::S_BYTES + r * 16 + (q & 7) * 2 + h);
+        lds_barrier();
+        cur = cur + 1 == C::NST ? 0 : cur + 1;
+        if ((s + 1) % C::SPC == 0) rbuf = rbuf == 2 ? 0 : rbuf + 1;
+    };
+    // copy u of slice s + NST - 1, into the place of slice s - 1
+    auto copy = [&](int s, int u) __attribute__((always_inline)) {
+        issue(s + C::NST - 1, base + (cur == 0 ? C::NST - 1 : cur - 1) * C::STAGE, u);
+    };
+    if (nk >= C::NST - 1) wait_vmcnt<C::PER * (C::NST - 2)>();
+    else wait_vmcnt<0>();
+    lds_barrier();
+    constexpr std::true_type MORE{};
+    constexpr std::false_type REST{};
+    if constexpr (C::X4) {
+        struct Frag { uint4 w[NW], x[C::FM]; uint32_t sw[NW], sx[C::FM]; } f0, f1;
+        auto read = [&](int s, int k, Frag& f, int u) __attribute__((always_inline)) {
+            if (u < NW) {
+                read_w(s, k, u, f.w[u], f.sw[u]);
+            } else {
+                const int i = u - NW;
+                f.x[i] = read_x(2 * k + h, i);
+                const int a0 = scale_at(s, k, 0), a1 = half_pair ? scale_at(s, k, 1) : a0;
+                f.sx[i] = byte((odd[i] ? a1 : a0) + (C::NB * C::BN + wm * C::WTM) * 16 + i * 512);
+            }
+        };
+        auto mma = [&](const Frag& f) __attribute__((always_inline)) {
+            return [&](int b, int i, int j) __attribute__((always_inline)) {
+                acc[b][i][j] = mfma_mx32(f.w[b * C::FN + j], f.sw[b * C::FN + j], f.x[i], f.sx[i], acc[b][i][j]);
+            };
+        };
+        constexpr int NR = NW + C::FM;
+#pragma unroll
+        for (int u = 0; u < NR; ++u) read(0, 0, f0, u);
+        int s = 0;
+        for (; s + C::NST - 1 < nk; ++s) {
+            step(mma(f0), NR + C::PER, [&](int u) __attribute__((always_inline)) {
+                if (u < NR) read(s, 1, f1, u);
+                else copy(s, u - NR);
+            });
+            next(s, MORE);
+            step(mma(f1), NR, [&](int u) __attribute__((always_inline)) { read(s + 1, 0, f0, u); });
+        }
+        for (; s < nk; ++s) {
+            step(mma(f0), NR, [&](int u) __attribute__((always_inline)) { read(s, 1, f1, u); });
+            const bool cut = s * 4 + 4 > nkb;   // a last half slice: zeros
+#pragma unroll
+            for (int f = 0; f < NW; ++f) {
+                f1.w[f] = cut ? zero16() : f1.w[f];
+                f1.sw[f] = cut ? 127u : f1.sw[f];
+            }
+#pragma unroll
+            for (int i = 0; i < C::FM; ++i) f1.sx[i] = cut ? 127u : f1.sx[i];
+            next(s, REST);   // behind the last slice: reads that nothing uses
+            step(mma(f1), NR, [&](int u) __attribute__((always_inline)) { read(s + 1, 0, f0, u); });
+        }
+    } else {
+        uint4 w[NW], wnext[NW], x0[C::FM], x1[C::FM];
+        uint32_t snext[NW];
+        float sc[NW];
+        // instruction q of the slice: values 8 q .. 8 q + 7 of both blocks
+        auto mma = [&](int q, const uint4 (&x)[C::FM]) __attribute__((always_inline)) {
+            return [&, q](int b, int i, int j) __attribute__((always_inline)) {
+                const uint4& v = w[b * C::FN + j];
+                const uint32_t c = q == 0 ? v.x : q == 1 ? v.y : q == 2 ? v.z : v.w;
+                acc[b][i][j] = mfma32x32x16(__builtin_bit_cast(bf16x8, mx::decode8(c, sc[b * C::FN + j])),
+                                            __builtin_bit_cast(bf16x8, x[i]), acc[b][i][j]);
+            };
+        };
+        auto read = [&](int s, int u) __attribute__((always_inline)) {   // of slice s: weights, first x
+            if (u < NW) read_w(s, 0, u, wnext[u], snext[u]);
+            else x0[u - NW] = read_x(4 * h, u - NW);
+        };
+        auto slice = [&](int s, auto more) __attribute__((always_inline)) {
+#pragma unroll
+            for (int f = 0; f < NW; ++f) {   // the weights read ahead come into use
+                w[f] = wnext[f];
+                sc[f] = mx::scale_value(snext[f]);
+            }
+            constexpr int P = decltype(more)::value ? C::PER : 0, P0 = P / 2;
+            step(mma(0, x0), C::FM + P0, [&](int u) __attribute__((always_inline)) {
+                if (u < C::FM) x1[u] = read_x(4 * h + 1, u);
+                else copy(s, u - C::FM);
+            });
+            step(mma(1, x1), C::FM + P - P0, [&](int u) __attribute__((always_inline)) {
+                if (u < C::FM) x0[u] = read_x(4 * h + 2, u);
+                else copy(s, u - C::FM + P0);
+            });
+            step(mma(2, x0), C::FM, [&](int u) __attribute__((always_inline)) { x1[u] = read_x(4 * h + 3, u); });
+            next(s, more);   // behind the last slice: reads that nothing uses
+            step(mma(3, x1), NW + C::FM, [&](int u) __attribute__((always_inline)) { read(s + 1, u); });
         };
 #pragma unroll
-        for (int k = 0; k < C::KP; ++k) {
-            uint4 w[C::NB][C::FN];
-            uint32_t sw[C::NB][C::FN];
-#pragma unroll
-            for (int b = 0; b < C::NB; ++b)
-#pragma unroll
-                for (int j = 0; j < C::FN; ++j) {
-                    const int n = b * C::BN + wn * C::WTN + j * 32 + l32;
-                    w[b][j] = ld16(Wt + PW::byte(n, 2 * k + h));
-                    sw[b][j] = scale(n, k, wodd[j]);
-                }
-            if constexpr (C::X4) {
-                uint4 xf[C::FM];
-                uint32_t sx[C::FM];
-#pragma unroll
-                for (int i = 0; i < C::FM; ++i) {
-                    const int m = wm * C::WTM + i * 32 + l32;
-                    xf[i] = ld16(X + PX::byte(m, 2 * k + h));
-                    sx[i] = scale(C::NB * C::BN + m, k, xodd[i]);
-                }
-#pragma unroll
-                for (int b = 0; b < C::NB; ++b)
-#pragma unroll
-                    for (int i = 0; i < C::FM; ++i)
-#pragma unroll
-                        for (int j = 0; j < C::FN; ++j)
-                            acc[b][i][j] = mfma_mx32(w[b][j], sw[b][j], xf[i], sx[i], acc[b][i][j]);
-            } else {
-                float sc[C::NB][C::FN];
-#pragma unroll
-                for (int b = 0; b < C::NB; ++b)
-#pragma unroll
-                    for (int j = 0; j < C::FN; ++j) sc[b][j] = mx::scale_value(sw[b][j]);
-#pragma unroll
-                for (int q = 0; q < 4; ++q) {
-                    bf16x8 xf[C::FM];
-#pragma unroll
-                    for (int i = 0; i < C::FM; ++i)
-                        xf[i] = __builtin_bit_cast(bf16x8, ld16(X + PX::byte(wm * C::WTM + i * 32 + l32, 4 * h + q)));
-#pragma unroll
-                    for (int b = 0; b < C::NB; ++b)
-#pragma unroll
-                        for (int j = 0; j < C::FN; ++j) {
-                            const uint32_t c = q == 0 ? w[b][j].x : q == 1 ? w[b][j].y : q == 2 ? w[b][j].z : w[b][j].w;
-                            const bf16x8 wf = __builtin_bit_cast(bf16x8, mx::decode8(c, sc[b][j]));
-#pragma unroll
-                            for (int i = 0; i < C::FM; ++i)
-                                acc[b][i][j] = mfma32x32x16(wf, xf[i], acc[b][i][j]);
-                        }
-                }
-            }
-        }
-        cur = cur + 1 == C::NST ? 0 : cur + 1;
-        nxt = nxt + 1 == C::NST ? 0 : nxt + 1;
-        if ((s + 1) % C::SPC == 0) rbuf = rbuf == 2 ? 0 : rbuf + 1;
+        for (int u = 0; u < NW + C::FM; ++u) read(0, u);
+        int s = 0;
+        for (; s + C::NST - 1 < nk; ++s) slice(s, MORE);
+        for (; s < nk; ++s) slice(s, REST);
     }
     const WaveCoord<C> wc;
 #pragma unroll
