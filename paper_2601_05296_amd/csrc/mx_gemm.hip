@@ -29,13 +29,14 @@ __device__ __forceinline__ i32x8 fp4_operand(const uint4& c) {
     return i32x8{(int)c.x, (int)c.y, (int)c.z, (int)c.w, 0, 0, 0, 0};
 }
 // Operand format 4 is e2m1. Lane L supplies row (column) L % 16 of block L / 16 (16x16x128),
-// or L % 32 of block L / 32 (32x32x64), and that block's scale byte in the low byte of its
-// scale register; results as for the bfloat16 instructions (all checked on the device).
+// or L % 32 of block L / 32 (32x32x64), and that block's scale in the low (or another) byte
+// of its scale register; results as for the bfloat16 instructions (all checked on the device).
 __device__ __forceinline__ f32x4 mfma_mx16(const uint4& p, uint32_t sp, const uint4& q, uint32_t sq, const f32x4& c) {
     return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(fp4_operand(p), fp4_operand(q), c, 4, 4, 0, (int)sp, 0, (int)sq);
 }
+template <int BYTE>   // of the scale registers
 __device__ __forceinline__ f32x16 mfma_mx32(const uint4& p, uint32_t sp, const uint4& q, uint32_t sq, const f32x16& c) {
-    return __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(fp4_operand(p), fp4_operand(q), c, 4, 4, 0, (int)sp, 0, (int)sq);
+    return __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(fp4_operand(p), fp4_operand(q), c, 4, 4, BYTE, (int)sp, BYTE, (int)sq);
 }
 
 // the activation of one sum (a pair of sums for SwiGLU), in float32
@@ -352,7 +353,8 @@ struct Place {
     }
 };
 
-template <class C>
+// ODD (4-bit rows): rows have an odd number of pairs of blocks, K / 64.
+template <class C, bool ODD>
 __global__ void __launch_bounds__(C::THREADS)
 mx_tile(const Args a) {
     extern __shared__ __attribute__((aligned(16))) char lds[];
@@ -366,9 +368,10 @@ mx_tile(const Args a) {
     using PX = Place<C::XROW>;
     using PW = Place<C::WROW>;
     // this lane's sources, one for each copy
-    const uint8_t *px[C::NCX], *pw[C::NCW], *ps;   // ps + pd[i]: scale row of copy i, from its dword on
-    int64_t pd[C::NCS];
-    int leads = 0;                // bit i: the scale row of this lane's copy i starts in the middle of a dword
+    const uint8_t *px[C::NCX], *pw[C::NCW], *ps[C::NCS];
+    // four bits for each scale copy: this lane's dword of a chunk, and whether the row starts in
+    // the middle of a dword. Dword d of row r lies in place d ^ (r / 8) % 4 of the row's four.
+    int pd = 0;
     int cx[C::NCX], cw[C::NCW];   // chunk inside the slice
 #pragma unroll
     for (int i = 0; i < C::NCX; ++i) {
@@ -393,21 +396,20 @@ mx_tile(const Args a) {
         const uint8_t* p;
         if (r < C::NB * C::BN) p = a.ws[C::NB == 2 ? r / C::BN : 0] + column(r) * nkb;
         else p = a.xs + x_row(a, t.off + t.m0 + min(r - C::NB * C::BN, t.mrows - 1)) * nkb;
-        const int lead = (int)(reinterpret_cast<uintptr_t>(p) & 2);
-        if (i == 0) ps = p - lead;
-        pd[i] = p - lead - ps;
-        leads |= (lead >> 1) << i;
+        const int lead = (int)(reinterpret_cast<uintptr_t>(p) & 2), d = (lane ^ (r >> 3)) & 3;
+        ps[i] = p - lead + d * 4;
+        pd |= (lead * 2 | d) << (4 * i);
     }
     const uint32_t base = lds_offset(lds), sbase = base + C::RING;
-    // copy i of this wave's of scale chunk c (past the row: its last dword again); dword d of
-    // row r lies in place d ^ (r / 8) % 4 of the row's four
-    auto issue_scales = [&](int i, int c, int buf) __attribute__((always_inline)) {
-        const uint8_t* p = ps;
+    // copy i of this wave's of scale chunk c into the buffer at `dst` (past the row: its last
+    // dword again; a select among array elements would go to memory, hence the sums)
+    auto copy_scales = [&](int i, int c, uint32_t dst) __attribute__((always_inline)) {
+        const uint8_t* p = ps[0];
 #pragma unroll
-        for (int q = 1; q < C::NCS; ++q) p += i == q ? pd[q] : 0;   // (a select of array elements goes to memory)
-        const int d = (lane ^ ((wv * C::NCS + i) * 2 + (lane >> 5))) & 3;
-        dma4(p + min(c * 16 + d * 4, (nkb + (leads >> i & 1) * 2 - 1) & ~3),
-             sbase + buf * C::S_BYTES + (wv * C::NCS + i) * 256);
+        for (int q = 1; q < C::NCS; ++q) p += i == q ? ps[q] - ps[0] : 0;
+        const int e = pd >> (4 * i);
+        const int last = ((nkb + (e >> 1 & 2) - 1) & ~3) - 4 * (e & 3);   // dword of the row
+        dma4(p + min(c * 16, last), dst + (wv * C::NCS + i) * 256);
     };
     int sbuf = 1;   // buffer of the chunk after the one that the slices being issued are in
     // copy u of this wave's C::PER of slice s, slices in order. With 4-bit rows the last slice
@@ -415,7 +417,7 @@ mx_tile(const Args a) {
     auto issue = [&](int s, uint32_t dst, int u) __attribute__((always_inline)) {
         const int cut = C::KP == 2 && s * 4 + 4 > nkb ? 2 : 8;
         if (u < C::NCP) {
-            issue_scales((s % C::SPC * C::NCP + u) * C::NCS / (C::SPC * C::NCP), s / C::SPC + 1, sbuf);
+            copy_scales((s % C::SPC * C::NCP + u) * C::NCS / (C::SPC * C::NCP), s / C::SPC + 1, sbase + sbuf * C::S_BYTES);
             if (u == C::NCP - 1 && (s + 1) % C::SPC == 0) sbuf = sbuf == 2 ? 0 : sbuf + 1;
         } else if (u < C::NCP + C::NCX) {
             const int i = u - C::NCP;
@@ -439,7 +441,7 @@ mx_tile(const Args a) {
     __syncthreads();                       // the tile lookup's words are free
     __builtin_amdgcn_s_waitcnt(0x0F70);    // vmcnt(0): only copies are outstanding from here on
 #pragma unroll
-    for (int i = 0; i < C::NCS; ++i) issue_scales(i, 0, 0);
+    for (int i = 0; i < C::NCS; ++i) copy_scales(i, 0, sbase);
     for (int s = 0; s < C::NST - 1 && s < nk; ++s)
 #pragma unroll
         for (int u = 0; u < C::PER; ++u) issue(s, base + s * C::STAGE, u);
@@ -506,47 +508,121 @@ mx_tile(const Args a) {
     constexpr std::true_type MORE{};
     constexpr std::false_type REST{};
     if constexpr (C::X4) {
-        struct Frag { uint4 w[NW], x[C::FM]; uint32_t sw[NW], sx[C::FM]; } f0, f1;
-        auto read = [&](int s, int k, Frag& f, int u) __attribute__((always_inline)) {
-            if (u < NW) {
-                read_w(s, k, u, f.w[u], f.sw[u]);
+        constexpr int NR = NW + C::FM;
+        struct Frag { uint4 w[NW], x[C::FM]; } f0, f1;        // of a slice's first and second pair
+        // scales of a slice for this lane's half: bytes 0 and 2 of each fragment's word
+        uint32_t sa[NR], sb[NR];
+        const int swz = ((l32 >> 3) & 3) << 2;
+        const int lw = (wn * C::WTN + l32) * 16 + swz, lx = (C::NB * C::BN + wm * C::WTM + l32) * 16 + swz;
+        auto read = [&](int pos, int k, Frag& f, int u) __attribute__((always_inline)) {
+            if (u < NW)
+                f.w[u] = ld16(lds + pos * C::STAGE + C::X_BYTES + PW::byte(wn * C::WTN + l32, 2 * k + h) +
+                              (u / C::FN * C::BN + u % C::FN * 32) * C::WROW);
+            else
+                f.x[u - NW] = ld16(lds + pos * C::STAGE + PX::byte(wm * C::WTM + l32, 2 * k + h) +
+                                   (u - NW) * 32 * C::XROW);
+        };
+        // scales of fragment u of slice q of the chunk at r (the next chunk's at rn). Rows that
+        // start in mid-dword: the upper half of this dword and the lower of the next.
+        auto read_scale = [&](int r, int rn, int q, int u) __attribute__((always_inline)) {
+            const int l = u < NW ? lw : lx;
+            const int n = (u < NW ? u / C::FN * C::BN + u % C::FN * 32 : (u - NW) * 32) * 16;
+            const char* p = lds + ((r + l) ^ (q << 2)) + n;
+            if constexpr (!ODD) {
+                return *reinterpret_cast<const uint32_t*>(p) >> (8 * h);
             } else {
-                const int i = u - NW;
-                f.x[i] = read_x(2 * k + h, i);
-                const int a0 = scale_at(s, k, 0), a1 = half_pair ? scale_at(s, k, 1) : a0;
-                f.sx[i] = byte((odd[i] ? a1 : a0) + (C::NB * C::BN + wm * C::WTM) * 16 + i * 512);
+                const bool mid = u < NW ? l32 & 1 : odd[u < NW ? 0 : u - NW];
+                const char* pn = lds + (q == 3 ? rn + l : (r + l) ^ ((q + 1) << 2)) + n;
+                const uint32_t lo = *reinterpret_cast<const uint16_t*>(mid ? p + 2 : p);
+                const uint32_t hi = *reinterpret_cast<const uint16_t*>(mid ? pn : p + 2);
+                return (lo | hi << 16) >> (8 * h);
             }
         };
-        auto mma = [&](const Frag& f) __attribute__((always_inline)) {
+        auto mma0 = [&](const uint32_t (&sc)[NR]) __attribute__((always_inline)) {
             return [&](int b, int i, int j) __attribute__((always_inline)) {
-                acc[b][i][j] = mfma_mx32(f.w[b * C::FN + j], f.sw[b * C::FN + j], f.x[i], f.sx[i], acc[b][i][j]);
+                acc[b][i][j] = mfma_mx32<0>(f0.w[b * C::FN + j], sc[b * C::FN + j], f0.x[i], sc[NW + i], acc[b][i][j]);
             };
         };
-        constexpr int NR = NW + C::FM;
-#pragma unroll
-        for (int u = 0; u < NR; ++u) read(0, 0, f0, u);
+        auto mma1 = [&](const uint32_t (&sc)[NR]) __attribute__((always_inline)) {
+            return [&](int b, int i, int j) __attribute__((always_inline)) {
+                acc[b][i][j] = mfma_mx32<2>(f1.w[b * C::FN + j], sc[b * C::FN + j], f1.x[i], sc[NW + i], acc[b][i][j]);
+            };
+        };
+        int r0 = C::RING, r1 = C::RING + C::S_BYTES, r2 = C::RING + 2 * C::S_BYTES;   // this chunk's scales, ...
+        auto turn = [&] { const int r = r0; r0 = r1; r1 = r2; r2 = r; };
         int s = 0;
-        for (; s + C::NST - 1 < nk; ++s) {
-            step(mma(f0), NR + C::PER, [&](int u) __attribute__((always_inline)) {
-                if (u < NR) read(s, 1, f1, u);
+        auto begin = [&] {   // scales and first pair of slice s
+            const int q = s % C::SPC;
+#pragma unroll
+            for (int u = 0; u < NR; ++u) { sa[u] = read_scale(r0, r1, q, u); read(s % C::NST, 0, f0, u); }
+        };
+        begin();
+        if constexpr (C::NST == C::SPC && C::NCP == 1) {
+            // Whole chunks of four slices, with a whole chunk behind: every place in the ring and
+            // every scale copy is known at compile time (a loop that finds them out slice by
+            // slice issues 200 other instructions beside 16 matrix instructions, more than
+            // their 512 cycles hide).
+            auto slice = [&](auto Q, int c, uint32_t (&sc)[NR], uint32_t (&sn)[NR]) __attribute__((always_inline)) {
+                constexpr int q = decltype(Q)::value, t = (q + 3) & 3;   // place of the slice copied
+                step(mma0(sc), NR + C::PER, [&](int u) __attribute__((always_inline)) {
+                    if (u < NR) {
+                        read(q, 1, f1, u);
+                    } else if (u == NR) {
+                        copy_scales(t * C::NCS / C::SPC, c + (q ? 2 : 1), base + (q ? r2 : r1));
+                    } else if (u - NR - 1 < C::NCX) {
+                        const int i = u - NR - 1;
+                        dma16(px[i], base + t * C::STAGE + (wv + i * C::NW) * 1024);
+                        px[i] += C::XROW;
+                    } else {
+                        const int i = u - NR - 1 - C::NCX;
+                        dma16(pw[i], base + t * C::STAGE + C::X_BYTES + (wv + i * C::NW) * 1024);
+                        pw[i] += C::WROW;
+                    }
+                });
+                wait_vmcnt<C::PER * (C::NST - 2)>();
+                lds_barrier();
+                step(mma1(sc), 2 * NR, [&](int u) __attribute__((always_inline)) {
+                    if (u < NR) read((q + 1) & 3, 0, f0, u);
+                    else sn[u - NR] = q == 3 ? read_scale(r1, r2, 0, u - NR) : read_scale(r0, r1, q + 1, u - NR);
+                });
+            };
+            for (; (s / 4 + 2) * 16 <= nkb; s += 4) {
+                slice(std::integral_constant<int, 0>{}, s / 4, sa, sb);
+                slice(std::integral_constant<int, 1>{}, s / 4, sb, sa);
+                slice(std::integral_constant<int, 2>{}, s / 4, sa, sb);
+                slice(std::integral_constant<int, 3>{}, s / 4, sb, sa);
+                turn();
+            }
+        }
+        // the rest, slice by slice
+        cur = s % C::NST;
+        sbuf = (r1 - C::RING) / C::S_BYTES;      // of the chunk after the one that slice s is in;
+        if (s % C::SPC + C::NST - 1 >= C::SPC) sbuf = sbuf == 2 ? 0 : sbuf + 1;   // slice s + NST - 1
+        auto rest = [&](auto more) __attribute__((always_inline)) {
+            constexpr int P = decltype(more)::value ? C::PER : 0;
+            step(mma0(sa), NR + P, [&](int u) __attribute__((always_inline)) {
+                if (u < NR) read(cur, 1, f1, u);
                 else copy(s, u - NR);
             });
-            next(s, MORE);
-            step(mma(f1), NR, [&](int u) __attribute__((always_inline)) { read(s + 1, 0, f0, u); });
-        }
-        for (; s < nk; ++s) {
-            step(mma(f0), NR, [&](int u) __attribute__((always_inline)) { read(s, 1, f1, u); });
-            const bool cut = s * 4 + 4 > nkb;   // a last half slice: zeros
+            if (s * 4 + 4 > nkb) {   // a last half slice: its second pair is zeros
 #pragma unroll
-            for (int f = 0; f < NW; ++f) {
-                f1.w[f] = cut ? zero16() : f1.w[f];
-                f1.sw[f] = cut ? 127u : f1.sw[f];
+                for (int u = 0; u < NW; ++u) f1.w[u] = zero16();
+#pragma unroll
+                for (int u = 0; u < NR; ++u) sa[u] = 127u << 16;
             }
+            next(s, more);
+            ++s;
+            if (s % C::SPC == 0) turn();
+            const int q = s % C::SPC;
+            step(mma1(sa), 2 * NR, [&](int u) __attribute__((always_inline)) {   // behind the last slice: not used
+                if (u < NR) read(cur, 0, f0, u);
+                else sb[u - NR] = read_scale(r0, r1, q, u - NR);
+            });
 #pragma unroll
-            for (int i = 0; i < C::FM; ++i) f1.sx[i] = cut ? 127u : f1.sx[i];
-            next(s, REST);   // behind the last slice: reads that nothing uses
-            step(mma(f1), NR, [&](int u) __attribute__((always_inline)) { read(s + 1, 0, f0, u); });
-        }
+            for (int u = 0; u < NR; ++u) sa[u] = sb[u];
+        };
+        while (s + C::NST - 1 < nk) rest(MORE);
+        while (s < nk) rest(REST);
     } else {
         uint4 w[NW], wnext[NW], x0[C::FM], x1[C::FM];
         uint32_t snext[NW];
@@ -635,13 +711,19 @@ hipError_t stream(const MxArgs& m, const Args& a, hipStream_t st) {
 template <class C>
 hipError_t tile(const MxArgs& m, const Args& a, hipStream_t st) {
     const int64_t grid = row_tiles(m.S, m.E, C::BM) * ((m.N + C::BN - 1) / C::BN);
-    static const hipError_t attr = hipFuncSetAttribute(
-        reinterpret_cast<const void*>(&mx_tile<C>), hipFuncAttributeMaxDynamicSharedMemorySize, C::LDS);
-    if (attr != hipSuccess) return attr;
     if (grid > INT32_MAX / C::THREADS) return hipErrorInvalidConfiguration;
-    hipLaunchKernelGGL(mx_tile<C>, dim3((unsigned)grid), dim3(C::THREADS), C::LDS, st, a);
-    probe::mark("mx_tile", st);
-    return hipGetLastError();
+    auto go = [&](auto odd) {
+        constexpr bool ODD = decltype(odd)::value;
+        static const hipError_t attr = hipFuncSetAttribute(
+            reinterpret_cast<const void*>(&mx_tile<C, ODD>), hipFuncAttributeMaxDynamicSharedMemorySize, C::LDS);
+        if (attr != hipSuccess) return attr;
+        hipLaunchKernelGGL((mx_tile<C, ODD>), dim3((unsigned)grid), dim3(C::THREADS), C::LDS, st, a);
+        probe::mark("mx_tile", st);
+        return hipGetLastError();
+    };
+    if constexpr (C::X4)
+        if (m.K / 64 % 2) return go(std::true_type{});
+    return go(std::false_type{});
 }
 
 // Times in us, bfloat16 rows, the alternatives on the same data.
