@@ -436,7 +436,8 @@ int moe_mx_dequantize(const void* codes, const void* scales, int64_t R, int K, u
  *      as moe_mx_quantize writes them; w, w3 [E,N,K/2] codes, w_scales, w3_scales
  *      [E,N,K/32] (w3 with MOE_GATED, else NULL); offsets [E+1], rows [S] int32.
  * Out: out [S,N] bfloat16. Rows at or behind offsets[E] are left as they were.
- * Limits: K and N multiples of 64, E <= 256, S < 2^31, T < 2^31; rows NULL: T == S.
+ * Limits: K and N multiples of 64, N K < 2^33, E <= 256, S < 2^31, T < 2^31; rows
+ * NULL: T == S.
  * The scales 0 to 254 stand for 2^(s - 127), 255 for NaN. Scales are read in
  * whole aligned 4-byte words: where T K/32 is not a multiple of 4, up to two
  * bytes behind the last of x_scales are read (and not used). No workspace.

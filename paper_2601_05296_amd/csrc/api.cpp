@@ -688,6 +688,8 @@ int moe_mx_gemm(const void* x, const void* x_scales, const void* w, const void* 
     if ((r = check_dim(fn, "K", K)) || (r = check_dim(fn, "N", N))) return r;
     if (S >= (int64_t(1) << 31) || T >= (int64_t(1) << 31))
         return fail(MOE_ERR_UNSUPPORTED, "%s: T = %lld, S = %lld do not fit int32", fn, (long long)T, (long long)S);
+    if ((int64_t)N * K >= (int64_t(1) << 33))
+        return fail(MOE_ERR_UNSUPPORTED, "%s: N * K = %lld, 2^33 or more", fn, (long long)N * K);
     if (!rows && S != T) return fail(MOE_ERR_INVALID_ARG, "%s: rows is NULL and T = %lld is not S = %lld", fn, (long long)T, (long long)S);
     if (S > 0 && T == 0) return fail(MOE_ERR_INVALID_ARG, "%s: T = 0 with S = %lld slots", fn, (long long)S);
     if (S == 0) return MOE_OK;

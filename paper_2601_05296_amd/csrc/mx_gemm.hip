@@ -290,9 +290,9 @@ mx_stream(const Args a) {
 
 // ---- tile core --------------------------------------------------------------------------
 // BM x BN outputs of NB weights, WM x WN waves of 32 x 32 fragments. A slice is 64 values of
-// K with bfloat16 rows (128-byte rows of x, 32-byte rows of codes), 128 with 4-bit rows
-// (64-byte rows of either). Each 64 values are two blocks; lane half h = L / 32 takes block h
-// of them, one 16-byte LDS read of codes, which four 32x32x16 bfloat16 or one 32x32x64
+// K with bfloat16 rows (128-byte rows of x, 32-byte rows of codes), 256 with 4-bit rows
+// (128-byte rows of either: whole lines take 40% fewer requests to L2 than slices of 128 do).
+// Each 64 values are two blocks; lane half h = L / 32 takes block h of them, one 16-byte LDS read of codes, which four 32x32x16 bfloat16 or one 32x32x64
 // scaled instruction use up. With bfloat16 rows instruction q takes values 8q .. 8q + 7 of
 // both blocks, so x comes as the chunks at bytes 64 h + 16 q of its row.
 // Scales come for 512 values of K at a time, 16 bytes of each row as aligned dwords, four
@@ -303,6 +303,12 @@ mx_stream(const Args a) {
 // middle of a dword: their chunks begin two bytes early. (The last dword of all may end two
 // bytes behind the last scale of x; those bytes are not used.)
 
+// 16-byte global -> LDS copy as dma16 (gemm.hpp), from a base of the whole wave's and a lane's
+// offset
+__device__ __forceinline__ void dma16_at(const void* base, uint32_t off, uint32_t lds_off) {
+    asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %1"
+                 ::"v"(off), "s"(base), "s"(lds_off) : "memory", "m0");
+}
 // 4-byte global -> LDS copy: lane l writes the dword at lds_off + 4 l
 __device__ __forceinline__ void dma4(const void* g, uint32_t lds_off) {
     asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dword %0, off"
@@ -315,9 +321,9 @@ struct TCfg {
     static constexpr bool X4 = X4_;
     static constexpr int NW = WM * WN, THREADS = 64 * NW;
     static constexpr int WTM = BM / WM, WTN = BN / WN, FM = WTM / 32, FN = WTN / 32;
-    static constexpr int KS = X4 ? 128 : 64;              // values of a slice
+    static constexpr int KS = X4 ? 256 : 64;              // values of a slice
     static constexpr int KP = KS / 64;                    // pairs of blocks
-    static constexpr int XROW = X4 ? 64 : 128, WROW = KS / 2;
+    static constexpr int XROW = 128, WROW = KS / 2;
     static constexpr int X_BYTES = BM * XROW, W_BYTES = NB * BN * WROW;
     static constexpr int NCX = X_BYTES / 1024 / NW, NCW = W_BYTES / 1024 / NW;
     // scale rows: the weights' NB * BN, then (4-bit rows) x's BM; chunks of 16 bytes each
@@ -328,6 +334,7 @@ struct TCfg {
     static constexpr int STAGE = X_BYTES + W_BYTES, RING = NST * STAGE;
     static constexpr int LDS = RING + 3 * S_BYTES;
     static constexpr int PER = NCX + NCW + NCP;
+    static constexpr int AHEAD = X4 ? (PER + 2) / 3 : 0;       // copies of a slice that go out two slices ahead
     static_assert(SROWS % (16 * NW) == 0 && NST <= SPC + 1, "scale rows, buffers");
     static_assert(X_BYTES % (1024 * NW) == 0 && W_BYTES % (1024 * NW) == 0 && NCX >= 1 && NCW >= 1, "copies");
     static_assert(FM >= 1 && FN >= 1 && LDS <= 160 * 1024 && PER * (NST - 1) < 64, "tile");
@@ -368,33 +375,41 @@ mx_tile(const Args a) {
     using PX = Place<C::XROW>;
     using PW = Place<C::WROW>;
     // this lane's sources, one for each copy
-    const uint8_t *px[C::NCX], *pw[C::NCW], *ps[C::NCS];
+    const uint8_t *px[C::NCX], *ps[C::NCS];
     // four bits for each scale copy: this lane's dword of a chunk, and whether the row starts in
     // the middle of a dword. Dword d of row r lies in place d ^ (r / 8) % 4 of the row's four.
     int pd = 0;
-    int cx[C::NCX], cw[C::NCW];   // chunk inside the slice
+    uint32_t ow[C::NCW];          // offsets into the expert's matrix (below 4 GB: N K < 2^33)
+    const uint8_t* bw[C::NB];     // and its start, moved on with the slices
+    auto chunk_x = [&](int i, int& r) { int c; PX::at((wv + i * C::NW) * 64 + lane, r, c); return c; };
+    auto chunk_w = [&](int i, int& r) { int c; PW::at((wv + i * C::NW) * 64 + lane, r, c); return c; };
 #pragma unroll
     for (int i = 0; i < C::NCX; ++i) {
         int r;
-        PX::at((wv + i * C::NW) * 64 + lane, r, cx[i]);
+        const int c = chunk_x(i, r);
         const int64_t row = x_row(a, t.off + t.m0 + min(r, t.mrows - 1));
-        px[i] = static_cast<const uint8_t*>(a.x) + row * (C::X4 ? a.K / 2 : 2 * a.K) + cx[i] * 16;
+        px[i] = static_cast<const uint8_t*>(a.x) + row * (C::X4 ? a.K / 2 : 2 * a.K) + c * 16;
     }
-    auto column = [&](int n) {   // of tile column n over the NB weights, clamped
-        return (int64_t)t.e * a.N + min(t.n0 + n % C::BN, a.N - 1);
-    };
+    auto column = [&](int n) { return min(t.n0 + n % C::BN, a.N - 1); };   // of weight row n of the tile
+#pragma unroll
+    for (int b = 0; b < C::NB; ++b) bw[b] = a.w[b] + (int64_t)t.e * a.N * (a.K / 2);
 #pragma unroll
     for (int i = 0; i < C::NCW; ++i) {
         int r;
-        PW::at((wv + i * C::NW) * 64 + lane, r, cw[i]);
-        pw[i] = a.w[C::NB == 2 ? r / C::BN : 0] + column(r) * (a.K / 2) + cw[i] * 16;
+        const int c = chunk_w(i, r);
+        ow[i] = (uint32_t)column(r) * (uint32_t)(a.K / 2) + c * 16;
     }
+    // the start of the weight that copy i of this wave belongs to
+    auto weight = [&](int i) __attribute__((always_inline)) {
+        if constexpr (C::NB == 1) return bw[0];
+        else return (wv + i * C::NW) * 1024 >= C::BN * C::WROW ? bw[1] : bw[0];
+    };
     const int half_pair = nkb & 2;   // rows start in the middle of a dword every other time
 #pragma unroll
     for (int i = 0; i < C::NCS; ++i) {
         const int r = (wv * C::NCS + i) * 16 + (lane >> 2);
         const uint8_t* p;
-        if (r < C::NB * C::BN) p = a.ws[C::NB == 2 ? r / C::BN : 0] + column(r) * nkb;
+        if (r < C::NB * C::BN) p = a.ws[C::NB == 2 ? r / C::BN : 0] + ((int64_t)t.e * a.N + column(r)) * nkb;
         else p = a.xs + x_row(a, t.off + t.m0 + min(r - C::NB * C::BN, t.mrows - 1)) * nkb;
         const int lead = (int)(reinterpret_cast<uintptr_t>(p) & 2), d = (lane ^ (r >> 3)) & 3;
         ps[i] = p - lead + d * 4;
@@ -412,21 +427,25 @@ mx_tile(const Args a) {
         dma4(p + min(c * 16, last), dst + (wv * C::NCS + i) * 256);
     };
     int sbuf = 1;   // buffer of the chunk after the one that the slices being issued are in
-    // copy u of this wave's C::PER of slice s, slices in order. With 4-bit rows the last slice
-    // may be half a slice: its second half, which is not used, comes from the first.
+    // copy u of this wave's C::PER of slice s, slices in order (4-bit rows: of slice 0, which K
+    // may cut short: chunk 0 stands in for those behind K, which are not used)
     auto issue = [&](int s, uint32_t dst, int u) __attribute__((always_inline)) {
-        const int cut = C::KP == 2 && s * 4 + 4 > nkb ? 2 : 8;
+        int r;
         if (u < C::NCP) {
             copy_scales((s % C::SPC * C::NCP + u) * C::NCS / (C::SPC * C::NCP), s / C::SPC + 1, sbase + sbuf * C::S_BYTES);
             if (u == C::NCP - 1 && (s + 1) % C::SPC == 0) sbuf = sbuf == 2 ? 0 : sbuf + 1;
         } else if (u < C::NCP + C::NCX) {
             const int i = u - C::NCP;
-            dma16(px[i] - (cx[i] >= cut ? 32 : 0), dst + (wv + i * C::NW) * 1024);
+            const int c = chunk_x(i, r);
+            dma16(px[i] - (C::X4 && c >= nkb ? c * 16 : 0), dst + (wv + i * C::NW) * 1024);
             px[i] += C::XROW;
         } else {
             const int i = u - C::NCP - C::NCX;
-            dma16(pw[i] - (cw[i] >= cut ? 32 : 0), dst + C::X_BYTES + (wv + i * C::NW) * 1024);
-            pw[i] += C::WROW;
+            const int c = chunk_w(i, r);
+            dma16_at(weight(i), ow[i] - (C::X4 && c >= nkb ? c * 16 : 0), dst + C::X_BYTES + (wv + i * C::NW) * 1024);
+            if (u == C::PER - 1)
+#pragma unroll
+                for (int b = 0; b < C::NB; ++b) bw[b] += C::WROW;
         }
     };
     f32x16 acc[C::NB][C::FM][C::FN];
@@ -505,8 +524,6 @@ mx_tile(const Args a) {
     if (nk >= C::NST - 1) wait_vmcnt<C::PER * (C::NST - 2)>();
     else wait_vmcnt<0>();
     lds_barrier();
-    constexpr std::true_type MORE{};
-    constexpr std::false_type REST{};
     if constexpr (C::X4) {
         constexpr int NR = NW + C::FM;
         struct Frag { uint4 w[NW], x[C::FM]; } f0, f1;        // of a slice's first and second pair
@@ -538,92 +555,109 @@ mx_tile(const Args a) {
                 return (lo | hi << 16) >> (8 * h);
             }
         };
-        auto mma0 = [&](const uint32_t (&sc)[NR]) __attribute__((always_inline)) {
-            return [&](int b, int i, int j) __attribute__((always_inline)) {
-                acc[b][i][j] = mfma_mx32<0>(f0.w[b * C::FN + j], sc[b * C::FN + j], f0.x[i], sc[NW + i], acc[b][i][j]);
-            };
-        };
-        auto mma1 = [&](const uint32_t (&sc)[NR]) __attribute__((always_inline)) {
-            return [&](int b, int i, int j) __attribute__((always_inline)) {
-                acc[b][i][j] = mfma_mx32<2>(f1.w[b * C::FN + j], sc[b * C::FN + j], f1.x[i], sc[NW + i], acc[b][i][j]);
-            };
-        };
         int r0 = C::RING, r1 = C::RING + C::S_BYTES, r2 = C::RING + 2 * C::S_BYTES;   // this chunk's scales, ...
         auto turn = [&] { const int r = r0; r0 = r1; r1 = r2; r2 = r; };
-        int s = 0;
-        auto begin = [&] {   // scales and first pair of slice s
-            const int q = s % C::SPC;
-#pragma unroll
-            for (int u = 0; u < NR; ++u) { sa[u] = read_scale(r0, r1, q, u); read(s % C::NST, 0, f0, u); }
-        };
-        begin();
-        if constexpr (C::NST == C::SPC && C::NCP == 1) {
-            // Whole chunks of four slices, with a whole chunk behind: every place in the ring and
-            // every scale copy is known at compile time (a loop that finds them out slice by
-            // slice issues 200 other instructions beside 16 matrix instructions, more than
-            // their 512 cycles hide).
-            auto slice = [&](auto Q, int c, uint32_t (&sc)[NR], uint32_t (&sn)[NR]) __attribute__((always_inline)) {
-                constexpr int q = decltype(Q)::value, t = (q + 3) & 3;   // place of the slice copied
-                step(mma0(sc), NR + C::PER, [&](int u) __attribute__((always_inline)) {
-                    if (u < NR) {
-                        read(q, 1, f1, u);
-                    } else if (u == NR) {
-                        copy_scales(t * C::NCS / C::SPC, c + (q ? 2 : 1), base + (q ? r2 : r1));
-                    } else if (u - NR - 1 < C::NCX) {
-                        const int i = u - NR - 1;
-                        dma16(px[i], base + t * C::STAGE + (wv + i * C::NW) * 1024);
-                        px[i] += C::XROW;
-                    } else {
-                        const int i = u - NR - 1 - C::NCX;
-                        dma16(pw[i], base + t * C::STAGE + C::X_BYTES + (wv + i * C::NW) * 1024);
-                        pw[i] += C::WROW;
-                    }
-                });
-                wait_vmcnt<C::PER * (C::NST - 2)>();
-                lds_barrier();
-                step(mma1(sc), 2 * NR, [&](int u) __attribute__((always_inline)) {
-                    if (u < NR) read((q + 1) & 3, 0, f0, u);
-                    else sn[u - NR] = q == 3 ? read_scale(r1, r2, 0, u - NR) : read_scale(r0, r1, q + 1, u - NR);
-                });
+        auto mma = [&](const Frag& f, const uint32_t (&sc)[NR], auto BYTE) __attribute__((always_inline)) {
+            return [&](int b, int i, int j) __attribute__((always_inline)) {
+                acc[b][i][j] = mfma_mx32<decltype(BYTE)::value>(f.w[b * C::FN + j], sc[b * C::FN + j], f.x[i],
+                                                                sc[NW + i], acc[b][i][j]);
             };
-            for (; (s / 4 + 2) * 16 <= nkb; s += 4) {
-                slice(std::integral_constant<int, 0>{}, s / 4, sa, sb);
-                slice(std::integral_constant<int, 1>{}, s / 4, sb, sa);
-                slice(std::integral_constant<int, 2>{}, s / 4, sa, sb);
-                slice(std::integral_constant<int, 3>{}, s / 4, sb, sa);
-                turn();
-            }
-        }
-        // the rest, slice by slice
-        cur = s % C::NST;
-        sbuf = (r1 - C::RING) / C::S_BYTES;      // of the chunk after the one that slice s is in;
-        if (s % C::SPC + C::NST - 1 >= C::SPC) sbuf = sbuf == 2 ? 0 : sbuf + 1;   // slice s + NST - 1
-        auto rest = [&](auto more) __attribute__((always_inline)) {
-            constexpr int P = decltype(more)::value ? C::PER : 0;
-            step(mma0(sa), NR + P, [&](int u) __attribute__((always_inline)) {
-                if (u < NR) read(cur, 1, f1, u);
-                else copy(s, u - NR);
-            });
-            if (s * 4 + 4 > nkb) {   // a last half slice: its second pair is zeros
-#pragma unroll
-                for (int u = 0; u < NW; ++u) f1.w[u] = zero16();
-#pragma unroll
-                for (int u = 0; u < NR; ++u) sa[u] = 127u << 16;
-            }
-            next(s, more);
-            ++s;
-            if (s % C::SPC == 0) turn();
-            const int q = s % C::SPC;
-            step(mma1(sa), 2 * NR, [&](int u) __attribute__((always_inline)) {   // behind the last slice: not used
-                if (u < NR) read(cur, 0, f0, u);
-                else sb[u - NR] = read_scale(r0, r1, q, u - NR);
-            });
-#pragma unroll
-            for (int u = 0; u < NR; ++u) sa[u] = sb[u];
         };
-        while (s + C::NST - 1 < nk) rest(MORE);
-        while (s < nk) rest(REST);
+        constexpr std::integral_constant<int, 0> LO{};
+        constexpr std::integral_constant<int, 2> HI{};
+        static_assert(C::NST == 2 && C::SPC == 2 && C::KP == 4, "ring places and scale words of a slice");
+        int s = 0;
+        // copy u of slice s + d (Q, CUT: of slice s, below)
+        auto copy = [&](auto Q, auto CUT, int d, int u) __attribute__((always_inline)) {
+            constexpr bool CUTS = decltype(CUT)::value;
+            const int q = Q, place = d == 1 ? 1 - q : q;
+            // behind K: chunk 0 of its row, of the last slice where the slice does not exist
+            const int left = nkb - (s + d) * 8;
+            const int none = max(s + d - nk + 1, 0) * 128;
+            auto back = [&](int c) __attribute__((always_inline)) { return CUTS && c >= left ? c * 16 : 0; };
+            int r;
+            if (u < C::NCP) {
+                copy_scales((place * C::NCP + u) * C::NCS / (2 * C::NCP), (s + d) / 2 + 1,
+                            base + (d == 2 || q ? r2 : r1));
+            } else if (u < C::NCP + C::NCX) {
+                const int i = u - C::NCP;
+                dma16(px[i] - none - back(chunk_x(i, r)), base + place * C::STAGE + (wv + i * C::NW) * 1024);
+                px[i] += C::XROW;
+            } else {
+                const int i = u - C::NCP - C::NCX;
+                dma16_at(weight(i) - none, ow[i] - back(chunk_w(i, r)),
+                         base + place * C::STAGE + C::X_BYTES + (wv + i * C::NW) * 1024);
+                if (u == C::PER - 1)
+#pragma unroll
+                    for (int b = 0; b < C::NB; ++b) bw[b] += C::WROW;
+            }
+        };
+        // Slice s, number q = s % 2 of its scale chunk and in ring place q: four steps, the arrival
+        // of slice s + 1 before the last. Its copies go out beside the first two and the step
+        // behind the barrier before those: spread out, for a wave whose copy waits for the
+        // address unit issues no matrix instructions either. A scale word holds
+        // two pairs; words are read when those before them are used up. CUT: the slices behind may
+        // not exist, or slice s end early, with codes of zero and scales of 1.0 behind K then.
+        auto slice = [&](auto Q, auto CUT) __attribute__((always_inline)) {
+            const int q = Q, t = 1 - q;
+            constexpr bool CUTS = decltype(CUT)::value;
+            auto cut = [&](int k, Frag& f, uint32_t (&sc)[NR]) __attribute__((always_inline)) {
+                if constexpr (CUTS) {
+                    const bool past = s * 8 + k * 2 >= nkb;
+#pragma unroll
+                    for (int u = 0; u < NW; ++u) f.w[u] = past ? zero16() : f.w[u];
+#pragma unroll
+                    for (int u = 0; u < NR; ++u) sc[u] = past ? 0x007f007fu : sc[u];
+                }
+            };
+            constexpr int P0 = C::AHEAD, P1 = P0 + (C::PER - P0 + 1) / 2;
+            step(mma(f0, sa, LO), NR + P1 - P0, [&](int u) __attribute__((always_inline)) {
+                if (u < NR) read(q, 1, f1, u);
+                else copy(Q, CUT, 1, u - NR + P0);
+            });
+            cut(1, f1, sa);
+            constexpr int P2 = C::PER - P1;
+            step(mma(f1, sa, HI), 2 * NR + P2, [&](int u) __attribute__((always_inline)) {
+                if (u < NR) read(q, 2, f0, u);
+                else if (u < NR + P2) copy(Q, CUT, 1, u - NR + P1);
+                else sb[u - NR - P2] = read_scale(r0, r1, 2 * q + 1, u - NR - P2);
+            });
+            cut(2, f0, sb);
+            step(mma(f0, sb, LO), NR, [&](int u) __attribute__((always_inline)) { read(q, 3, f1, u); });
+            cut(3, f1, sb);
+            wait_vmcnt<0>();
+            lds_barrier();   // all waves have read slice s, and slice s + 1 is there for all
+            step(mma(f1, sb, HI), 2 * NR + P0, [&](int u) __attribute__((always_inline)) {
+                if (u < NR) read(t, 0, f0, u);
+                else if (u < 2 * NR) sa[u - NR] = read_scale(q ? r1 : r0, q ? r2 : r1, 2 * t, u - NR);
+                else copy(Q, CUT, 2, u - 2 * NR);
+            });
+        };
+#pragma unroll
+        for (int u = 0; u < NR; ++u) {
+            sa[u] = read_scale(r0, r1, 0, u);
+            read(0, 0, f0, u);
+        }
+#pragma unroll
+        for (int u = 0; u < C::AHEAD; ++u) copy(0, std::true_type{}, 1, u);
+        // Whole chunks of two slices, with whole slices or none behind: places and copies are
+        // known at compile time (a loop that finds them out slice by slice issues twice as many
+        // instructions beside the matrix instructions, more than those hide).
+        const int behind = nkb % 8 ? 2 : 1;
+        for (; (s / 2 + behind) * 16 <= nkb; turn()) {
+            slice(std::integral_constant<int, 0>{}, std::false_type{});
+            ++s;
+            slice(std::integral_constant<int, 1>{}, std::false_type{});
+            ++s;
+        }
+        for (; s < nk; ++s) {
+            slice(s & 1, std::true_type{});
+            if (s & 1) turn();
+        }
+        wait_vmcnt<0>();   // no copy may land behind the workgroup's end
     } else {
+        constexpr std::true_type MORE{};
+        constexpr std::false_type REST{};
         uint4 w[NW], wnext[NW], x0[C::FM], x1[C::FM];
         uint32_t snext[NW];
         float sc[NW];
@@ -732,8 +766,7 @@ hipError_t pick(const MxArgs& m, const Args& a, hipStream_t st) {
     // rows of an expert that has any, about, and workgroups of 64 columns
     const double rows = (double)m.S / (double)std::min<int64_t>(m.S, m.E);
     const int64_t blocks = row_tiles(m.S, m.E, 16) * (m.N / 64);
-    constexpr int BN = NB == 2 ? 128 : 256;
-    constexpr int NST = X4 ? 4 : 3;
+    constexpr int BN = NB == 2 ? 128 : 256, NST = X4 ? 2 : 3;
     // Fewer workgroups than CUs, a row or so each (single tokens): 16 columns, and slices of
     // 1024 values, four waves deep. d = 14336 -> 4096, two experts: 13.9 against 22.8;
     // 2880 -> 2880 gated, four experts: 11.0, 12.2.
@@ -752,7 +785,10 @@ hipError_t pick(const MxArgs& m, const Args& a, hipStream_t st) {
         if constexpr (NB == 2) return stream<SCfg<32, 64, 2, 2, 2, NB, X4, 2, 64>>(m, a, st);
         else return stream<SCfg<32, 128, 4, 2, 2, NB, X4, 2, 64>>(m, a, st);
     }
-    if (rows <= 64) return tile<TCfg<64, BN, 1, 4, NB, X4, 3>>(m, a, st);
+    if (rows <= 64) {
+        if constexpr (X4) return tile<TCfg<64, 128 / NB, 2, 2, NB, X4, NST>>(m, a, st);
+        else return tile<TCfg<64, BN, 1, 4, NB, X4, NST>>(m, a, st);
+    }
     if (rows <= 128) return tile<TCfg<128, BN, 2, 4, NB, X4, NST>>(m, a, st);
     return tile<TCfg<256, BN, 2, 4, NB, X4, NST>>(m, a, st);
 }

@@ -161,6 +161,7 @@ def test_mx_gemm_refusals():
     assert gemm(flags=B.MOE_GATED) == INV and b"w3 is NULL" in lib.moe_last_error()
     assert gemm(flags=B.MOE_GATED, w3=FAKE) == INV and b"w3_scales is NULL" in lib.moe_last_error()
     assert gemm(w3=FAKE) == INV and b"without MOE_GATED" in lib.moe_last_error()
+    assert gemm(N=1 << 20, K=1 << 13) == UNS
     assert gemm(S=1 << 31) == UNS and gemm(T=1 << 31) == UNS and gemm(S=-1) == INV
     assert gemm(rows=None) == INV and b"not S" in lib.moe_last_error()
     assert gemm(T=0) == INV and gemm(x=None) == INV and gemm(ws=None) == INV and gemm(off=None) == INV
