@@ -11,6 +11,7 @@ from __future__ import annotations
 import ctypes
 import functools
 import os
+from array import array
 
 import torch
 
@@ -384,19 +385,41 @@ def moe_route_bwd(d_gates, logits, topk_ids, gates, x, w_gate, T, d, E, k, flags
                                         workspace_bytes, _stream(stream)))
 
 
-def _here(*tensors):
-    """The tensors of a call have to be on torch's current device: the call goes to that
-    device's stream."""
-    dev = None
-    for t in tensors:
-        if t is None or isinstance(t, int):
+def _current() -> int:
+    """torch's current device (-2 before any GPU tensor exists)."""
+    if not torch.cuda.is_initialized():
+        return -2
+    return _device() if _device is not None else torch.cuda.current_device()
+
+
+def _args(dev: int, *specs):
+    """The addresses of the tensors in `specs`, (tensor, least elements, dtype, name) each
+    (None and raw addresses as they are), after all checks of the operators around the layer:
+    types and sizes first, then that each is dense and on the current device `dev`, to whose
+    stream the call goes."""
+    ptrs, odd = [], None
+    for t, n, dtype, name in specs:
+        if t is None or t.__class__ is int:
+            ptrs.append(t)
             continue
-        if dev is None:
-            if not t.is_cuda:
-                raise ValueError("tensor must be on the GPU")
-            dev = torch.cuda.current_device()
-        if t.get_device() != dev:
-            raise ValueError("tensor on %s, the current device is cuda:%d" % (t.device, dev))
+        if t.dtype != dtype:
+            raise ValueError("%s: dtype %s, expected %s" % (name, t.dtype, dtype))
+        if t.numel() < n:
+            raise ValueError("%s: %d elements, at least %d needed" % (name, t.numel(), n))
+        if odd is None and (t.get_device() != dev or not t.is_contiguous()):
+            odd = (t, name)
+        ptrs.append(t.data_ptr())
+    if odd is not None:
+        _misplaced(*odd, dev)
+    return ptrs
+
+
+def _misplaced(t, name, dev):
+    if not t.is_cuda:
+        raise ValueError("tensor must be on the GPU")
+    if t.get_device() != dev:
+        raise ValueError("%s: tensor on %s, the current device is cuda:%d" % (name, t.device, dev))
+    raise ValueError("tensor must be contiguous")
 
 
 def _gate_count(flags, T, d):
@@ -407,16 +430,11 @@ def _gate_count(flags, T, d):
 
 def moe_norm_fwd(res, y, gate, w_post, w_pre, res_scale, eps, T, d, flags, r, n, rstd_post=None,
                  rstd_pre=None, stream=None):
-    el, f32 = _elt(flags), torch.float32
-    for t, m, name in ((res, T * d, "res"), (y, T * d, "y"), (gate, _gate_count(flags, T, d), "gate"),
-                       (w_post, d, "w_post"), (w_pre, d, "w_pre"), (r, T * d, "r"), (n, T * d, "n")):
-        _need(t, m, name, el)
-    _need(rstd_post, T, "rstd_post", f32)
-    _need(rstd_pre, T, "rstd_pre", f32)
-    _here(res, y, gate, w_post, w_pre, r, n, rstd_post, rstd_pre)
-    _check(load_library().moe_norm_fwd(_ptr(res), _ptr(y), _ptr(gate), _ptr(w_post), _ptr(w_pre),
-                                       res_scale, eps, T, d, flags, _ptr(r), _ptr(n),
-                                       _ptr(rstd_post), _ptr(rstd_pre), _stream(stream)))
+    el, f32, m = _elt(flags), torch.float32, T * d
+    p = _args(_current(), (res, m, el, "res"), (y, m, el, "y"), (gate, _gate_count(flags, T, d), el, "gate"),
+              (w_post, d, el, "w_post"), (w_pre, d, el, "w_pre"), (r, m, el, "r"), (n, m, el, "n"),
+              (rstd_post, T, f32, "rstd_post"), (rstd_pre, T, f32, "rstd_pre"))
+    _check(load_library().moe_norm_fwd(*p[:5], res_scale, eps, T, d, flags, *p[5:], _stream(stream)))
 
 
 @functools.lru_cache(maxsize=256, typed=True)
@@ -426,24 +444,17 @@ def moe_norm_bwd_workspace_size(T, d, flags) -> int:
 
 def moe_norm_bwd(dr, dn, y, r, gate, w_post, w_pre, rstd_post, rstd_pre, res_scale, T, d, flags,
                  dres, dy, dgate, dw_post, dw_pre, workspace, workspace_bytes, stream=None):
-    el, f32 = _elt(flags), torch.float32
+    el, f32, m = _elt(flags), torch.float32, T * d
     ng = _gate_count(flags, T, d)
     full = flags & MOE_GATE_CHANNEL and flags & MOE_GATE_TOKEN
-    for t, m, name in ((dr, T * d, "dr"), (dn, T * d, "dn"), (y, T * d, "y"), (r, T * d, "r"),
-                       (gate, ng, "gate"), (w_post, d, "w_post"), (w_pre, d, "w_pre"),
-                       (dres, T * d, "dres"), (dy, T * d, "dy")):
-        _need(t, m, name, el)
-    for t, m, name in ((rstd_post, T, "rstd_post"), (rstd_pre, T, "rstd_pre"),
-                       (dw_post, d, "dw_post"), (dw_pre, d, "dw_pre")):
-        _need(t, m, name, f32)
-    _need(dgate, ng, "dgate", el if full else f32)
+    p = _args(_current(), (dr, m, el, "dr"), (dn, m, el, "dn"), (y, m, el, "y"), (r, m, el, "r"),
+              (gate, ng, el, "gate"), (w_post, d, el, "w_post"), (w_pre, d, el, "w_pre"),
+              (rstd_post, T, f32, "rstd_post"), (rstd_pre, T, f32, "rstd_pre"), (dres, m, el, "dres"),
+              (dy, m, el, "dy"), (dgate, ng, el if full else f32, "dgate"), (dw_post, d, f32, "dw_post"),
+              (dw_pre, d, f32, "dw_pre"))
     _need_bytes(workspace, workspace_bytes)
-    _here(dr, dn, y, r, gate, w_post, w_pre, rstd_post, rstd_pre, dres, dy, dgate, dw_post, dw_pre,
-          workspace)
-    _check(load_library().moe_norm_bwd(
-        _ptr(dr), _ptr(dn), _ptr(y), _ptr(r), _ptr(gate), _ptr(w_post), _ptr(w_pre),
-        _ptr(rstd_post), _ptr(rstd_pre), res_scale, T, d, flags, _ptr(dres), _ptr(dy), _ptr(dgate),
-        _ptr(dw_post), _ptr(dw_pre), _ptr(workspace), workspace_bytes, _stream(stream)))
+    _check(load_library().moe_norm_bwd(*p[:9], res_scale, T, d, flags, *p[9:], _ptr(workspace),
+                                       workspace_bytes, _stream(stream)))
 
 
 @functools.lru_cache(maxsize=256, typed=True)
@@ -452,78 +463,71 @@ def moe_grad_norm_workspace_size(n) -> int:
 
 
 class TensorList:
-    """The host arrays (pointers, element counts, types) that the gradient calls take of a
-    list of contiguous bfloat16 and float32 tensors."""
+    """The host arrays (addresses, element counts, types) that the gradient calls take of a
+    list of contiguous bfloat16 and float32 tensors. The tensors have to live on, in place."""
 
     def __init__(self, tensors):
-        self.tensors = list(tensors)
-        _here(*self.tensors)
-        n = len(self.tensors)
-        self.n = n
-        self.ptrs = (ctypes.c_void_p * n)(*[_ptr(t) for t in self.tensors])
-        self.sizes = (ctypes.c_int64 * n)(*[t.numel() for t in self.tensors])
-        self.types = (ctypes.c_uint * n)(*[dtype_flag(t) for t in self.tensors])
+        self.tensors = tensors = list(tensors)
+        dev, f32, bf16 = _current(), torch.float32, torch.bfloat16
+        ptrs, sizes, types = [], [], []
+        for t in tensors:
+            dt = t.dtype
+            if dt is f32:
+                types.append(MOE_F32)
+            elif dt is bf16:
+                types.append(MOE_BF16)
+            else:
+                raise ValueError("unsupported dtype %s" % dt)
+            if t.get_device() != dev or not t.is_contiguous():
+                _misplaced(t, "gradient", dev)
+            ptrs.append(t.data_ptr())
+            sizes.append(t.numel())
+        self.n = len(tensors)
+        self.ptrs, self.sizes, self.types = array("Q", ptrs), array("q", sizes), array("I", types)
+
+    def addresses(self):
+        return (self.ptrs.buffer_info()[0], self.sizes.buffer_info()[0], self.types.buffer_info()[0])
 
 
 def moe_grad_norm(grads: TensorList, sumsq, norm, workspace, workspace_bytes, stream=None):
-    _need(sumsq, 1, "sumsq", torch.float64)
-    _need(norm, 1, "norm", torch.float32)
+    ps, pn = _args(_current(), (sumsq, 1, torch.float64, "sumsq"), (norm, 1, torch.float32, "norm"))
     _need_bytes(workspace, workspace_bytes)
-    _here(sumsq, norm, workspace)
-    _check(load_library().moe_grad_norm(grads.ptrs, grads.sizes, grads.types, grads.n, _ptr(sumsq),
-                                        _ptr(norm), _ptr(workspace), workspace_bytes,
-                                        _stream(stream)))
+    _check(load_library().moe_grad_norm(*grads.addresses(), grads.n, ps, pn, _ptr(workspace),
+                                        workspace_bytes, _stream(stream)))
 
 
 def moe_grad_clip(grads: TensorList, outs, sumsq, max_norm, stream=None):
     """`outs`: a TensorList of the same sizes and types, or None (in place)."""
-    _need(sumsq, 1, "sumsq", torch.float64)
-    _here(sumsq)
-    if outs is not None:
-        if list(outs.sizes) != list(grads.sizes) or list(outs.types) != list(grads.types):
-            raise ValueError("outs: not the gradients' sizes and types")
-    _check(load_library().moe_grad_clip(grads.ptrs, None if outs is None else outs.ptrs, grads.sizes,
-                                        grads.types, grads.n, _ptr(sumsq), max_norm,
-                                        _stream(stream)))
+    ps, = _args(_current(), (sumsq, 1, torch.float64, "sumsq"))
+    if outs is not None and (outs.sizes != grads.sizes or outs.types != grads.types):
+        raise ValueError("outs: not the gradients' sizes and types")
+    p, sizes, types = grads.addresses()
+    _check(load_library().moe_grad_clip(p, None if outs is None else outs.addresses()[0], sizes, types,
+                                        grads.n, ps, max_norm, _stream(stream)))
 
 
 def moe_mx_quantize(src, batch, R, K, flags, codes, scales, stream=None):
-    n = batch * R * K
-    _need(src, n, "src", _elt(flags))
-    _need(codes, n // 2, "codes", torch.uint8)
-    _need(scales, n // 32, "scales", torch.uint8)
-    _here(src, codes, scales)
-    _check(load_library().moe_mx_quantize(_ptr(src), batch, R, K, flags, _ptr(codes), _ptr(scales),
-                                          _stream(stream)))
+    n, u8 = batch * R * K, torch.uint8
+    p = _args(_current(), (src, n, _elt(flags), "src"), (codes, n // 2, u8, "codes"),
+              (scales, n // 32, u8, "scales"))
+    _check(load_library().moe_mx_quantize(p[0], batch, R, K, flags, p[1], p[2], _stream(stream)))
 
 
 def moe_mx_dequantize(codes, scales, R, K, flags, out, stream=None):
-    _need(codes, R * K // 2, "codes", torch.uint8)
-    _need(scales, R * K // 32, "scales", torch.uint8)
-    _need(out, R * K, "out", _elt(flags))
-    _here(codes, scales, out)
-    _check(load_library().moe_mx_dequantize(_ptr(codes), _ptr(scales), R, K, flags, _ptr(out),
-                                            _stream(stream)))
+    n, u8 = R * K, torch.uint8
+    p = _args(_current(), (codes, n // 2, u8, "codes"), (scales, n // 32, u8, "scales"),
+              (out, n, _elt(flags), "out"))
+    _check(load_library().moe_mx_dequantize(p[0], p[1], R, K, flags, p[2], _stream(stream)))
 
 
 def moe_mx_gemm(x, x_scales, w, w_scales, w3, w3_scales, offsets, rows, T, S, K, N, E, flags, out,
                 stream=None):
-    u8 = torch.uint8
-    if x_scales is None:
-        _need(x, T * K, "x", torch.bfloat16)
-    else:
-        _need(x, T * K // 2, "x", u8)
-        _need(x_scales, T * K // 32, "x_scales", u8)
-    for t, m, name in ((w, E * N * K // 2, "w"), (w_scales, E * N * K // 32, "w_scales"),
-                       (w3, E * N * K // 2, "w3"), (w3_scales, E * N * K // 32, "w3_scales")):
-        _need(t, m, name, u8)
-    _need(offsets, E + 1, "offsets", torch.int32)
-    _need(rows, S, "rows", torch.int32)
-    _need(out, S * N, "out", torch.bfloat16)
-    _here(x, x_scales, w, w_scales, w3, w3_scales, offsets, rows, out)
-    _check(load_library().moe_mx_gemm(_ptr(x), _ptr(x_scales), _ptr(w), _ptr(w_scales), _ptr(w3),
-                                      _ptr(w3_scales), _ptr(offsets), _ptr(rows), T, S, K, N, E,
-                                      flags, _ptr(out), _stream(stream)))
+    u8, i32, m, mx = torch.uint8, torch.int32, E * N * K, x_scales is not None
+    p = _args(_current(), (x, T * K // 2 if mx else T * K, u8 if mx else torch.bfloat16, "x"),
+              (x_scales, T * K // 32, u8, "x_scales"), (w, m // 2, u8, "w"), (w_scales, m // 32, u8, "w_scales"),
+              (w3, m // 2, u8, "w3"), (w3_scales, m // 32, u8, "w3_scales"), (offsets, E + 1, i32, "offsets"),
+              (rows, S, i32, "rows"), (out, S * N, torch.bfloat16, "out"))
+    _check(load_library().moe_mx_gemm(*p[:8], T, S, K, N, E, flags, p[8], _stream(stream)))
 
 
 def moe_probe_enable(capacity: int):

@@ -44,23 +44,36 @@ def _flags(t, gate, w_post, w_pre):
     return fl
 
 
+def _at(t):
+    return None if t is None else t.data_ptr()
+
+
 def norm_forward(res, y=None, gate=None, w_post=None, w_pre=None, res_scale: float = 1.0,
                  eps: float = 1e-6, keep: bool = True, stream=None) -> Normed:
     """r = res_scale * res + gate * post_norm(y), n = pre_norm(r) (moe_norm_fwd). ``res``,
     ``y`` [T, d]; ``gate`` [d], [T, 1], [T, d] or None; ``w_post``, ``w_pre`` [d], None
     where that norm is off. Without ``y``: n = pre_norm(res). ``keep`` False (inference)
     leaves out what only the backward needs."""
+    if stream is not None:
+        with _on(stream):
+            return norm_forward(res, y, gate, w_post, w_pre, res_scale, eps, keep)
     T, d = res.shape
     if y is not None and y.shape != res.shape:
         raise ValueError("y: %s, res is %s" % (tuple(y.shape), tuple(res.shape)))
-    fl = _flags(res, gate, w_post, w_pre)
-    with _on(stream):
-        dev = res.device
-        r = torch.empty_like(res) if y is not None else None
-        n = torch.empty_like(res) if w_pre is not None else None
-        po = torch.empty(T, dtype=torch.float32, device=dev) if keep and w_post is not None else None
-        pr = torch.empty(T, dtype=torch.float32, device=dev) if keep and w_pre is not None else None
-        B.moe_norm_fwd(res, y, gate, w_post, w_pre, res_scale, eps, T, d, fl, r, n, po, pr, None)
+    fl, el, dev, empty = _flags(res, gate, w_post, w_pre), res.dtype, res.device, torch.empty
+    ins = B._args(B._current(), (res, 0, el, "res"), (y, 0, el, "y"), (gate, 0, el, "gate"),
+                  (w_post, d, el, "w_post"), (w_pre, d, el, "w_pre"))
+    r = n = po = pr = None
+    if y is not None:
+        r = empty((T, d), dtype=el, device=dev)
+    if w_pre is not None:
+        n = empty((T, d), dtype=el, device=dev)
+    if keep and w_post is not None:
+        po = empty(T, dtype=torch.float32, device=dev)
+    if keep and w_pre is not None:
+        pr = empty(T, dtype=torch.float32, device=dev)
+    B._check(B.load_library().moe_norm_fwd(*ins, res_scale, eps, T, d, fl, _at(r), _at(n), _at(po), _at(pr),
+                                           B._stream(None)))
     return Normed(r, n, po, pr)
 
 
@@ -71,6 +84,9 @@ def norm_backward(dr, dn, y, r, rstd_post, rstd_pre, gate=None, w_post=None, w_p
     used further; ``dn`` None without ``w_pre``). ``r``: the forward's, or ``res`` where it
     had no ``y`` (``block`` False). dw_post, dw_pre and a channel's or token's dgate are
     float32, the rest of the inputs' type."""
+    if stream is not None:
+        with _on(stream):
+            return norm_backward(dr, dn, y, r, rstd_post, rstd_pre, gate, w_post, w_pre, res_scale, block)
     t = dr if dr is not None else dn
     if t is None:
         raise ValueError("neither dr nor dn")
@@ -78,20 +94,24 @@ def norm_backward(dr, dn, y, r, rstd_post, rstd_pre, gate=None, w_post=None, w_p
     for v, name in ((dr, "dr"), (dn, "dn"), (y, "y"), (r, "r")):
         if v is not None and v.shape != t.shape:
             raise ValueError("%s: %s, expected %s" % (name, tuple(v.shape), tuple(t.shape)))
-    fl = _flags(t, gate, w_post, w_pre)
-    with _on(stream):
-        dev, f32 = t.device, torch.float32
-        dres = torch.empty_like(t, memory_format=torch.contiguous_format)
-        dy = torch.empty_like(dres) if block else None
-        dgate = None
-        if gate is not None:
-            dgate = torch.empty(gate.shape, dtype=t.dtype if gate.shape == t.shape else f32, device=dev)
-        dwo = torch.empty(d, dtype=f32, device=dev) if w_post is not None else None
-        dwr = torch.empty(d, dtype=f32, device=dev) if w_pre is not None else None
-        wsb = B.moe_norm_bwd_workspace_size(T, d, fl)
-        ws = torch.empty(max(wsb, 16), dtype=torch.uint8, device=dev)
-        B.moe_norm_bwd(dr, dn, y, r, gate, w_post, w_pre, rstd_post, rstd_pre, res_scale, T, d, fl,
-                       dres, dy, dgate, dwo, dwr, ws, wsb, None)
+    fl, el, dev, f32, empty = _flags(t, gate, w_post, w_pre), t.dtype, t.device, torch.float32, torch.empty
+    ins = B._args(B._current(), (dr, 0, el, "dr"), (dn, 0, el, "dn"), (y, 0, el, "y"), (r, 0, el, "r"),
+                  (gate, 0, el, "gate"), (w_post, d, el, "w_post"), (w_pre, d, el, "w_pre"),
+                  (rstd_post, T, f32, "rstd_post"), (rstd_pre, T, f32, "rstd_pre"))
+    dres = empty((T, d), dtype=el, device=dev)
+    dy = dgate = dwo = dwr = None
+    if block:
+        dy = empty((T, d), dtype=el, device=dev)
+    if gate is not None:
+        dgate = empty(gate.shape, dtype=el if gate.shape == t.shape else f32, device=dev)
+    if w_post is not None:
+        dwo = empty(d, dtype=f32, device=dev)
+    if w_pre is not None:
+        dwr = empty(d, dtype=f32, device=dev)
+    wsb = B.moe_norm_bwd_workspace_size(T, d, fl)
+    ws = empty(max(wsb, 16), dtype=torch.uint8, device=dev)
+    B._check(B.load_library().moe_norm_bwd(*ins, res_scale, T, d, fl, dres.data_ptr(), _at(dy), _at(dgate),
+                                           _at(dwo), _at(dwr), ws.data_ptr(), wsb, B._stream(None)))
     return dict(dres=dres, dy=dy, dgate=dgate, dw_post=dwo, dw_pre=dwr)
 
 

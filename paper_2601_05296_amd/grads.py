@@ -13,13 +13,19 @@ def _list(grads):
     return [g for g in (grads.values() if isinstance(grads, dict) else grads) if g is not None]
 
 
-def _norm(tl, dev):
+def _norm(tl):
+    dev = _device(tl)
     norm = torch.empty((), dtype=torch.float32, device=dev)
     sumsq = torch.empty((), dtype=torch.float64, device=dev)
     wsb = B.moe_grad_norm_workspace_size(tl.n)
     ws = torch.empty(max(wsb, 16), dtype=torch.uint8, device=dev)
-    B.moe_grad_norm(tl, sumsq, norm, ws, wsb, None)
+    B._check(B.load_library().moe_grad_norm(*tl.addresses(), tl.n, sumsq.data_ptr(), norm.data_ptr(),
+                                            ws.data_ptr(), wsb, B._stream(None)))
     return norm, sumsq
+
+
+def _device(tl):
+    return tl.tensors[0].device if tl.n else torch.device("cuda", torch.cuda.current_device())
 
 
 def norm(grads, stream=None):
@@ -27,8 +33,7 @@ def norm(grads, stream=None):
     float64, both on the GPU. Where a model's gradients are spread over several devices the
     devices' sumsq add up."""
     with _on(stream):
-        tl = B.TensorList(_list(grads))
-        return _norm(tl, tl.tensors[0].device if tl.n else torch.device("cuda", torch.cuda.current_device()))
+        return _norm(B.TensorList(_list(grads)))
 
 
 def clip(grads, max_norm: float, out=None, sumsq=None, stream=None):
@@ -41,9 +46,8 @@ def clip(grads, max_norm: float, out=None, sumsq=None, stream=None):
         outs = None if out is None else B.TensorList(_list(out))
         if outs is not None and outs.n != tl.n:
             raise ValueError("out: %d tensors for %d gradients" % (outs.n, tl.n))
-        dev = tl.tensors[0].device if tl.n else torch.device("cuda", torch.cuda.current_device())
         if sumsq is None:
-            total, sumsq = _norm(tl, dev)
+            total, sumsq = _norm(tl)
         else:
             total = sumsq.sqrt().float()
         B.moe_grad_clip(tl, outs, sumsq, max_norm, None)

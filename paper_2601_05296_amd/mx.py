@@ -44,32 +44,44 @@ class MXExperts(NamedTuple):
 def quantize(x, transpose: bool = False, stream=None) -> MX:
     """``x`` [..., R, K] (bfloat16 or float32) in 4 bits, with a scale for each 32 values
     along K; with ``transpose`` of [..., K, R], whose result is laid out [..., R, K]."""
-    if x.dim() < 2:
-        raise ValueError("x: %d dimensions, at least 2 needed" % x.dim())
-    R, K = x.shape[-2:]
+    if stream is not None:
+        with _on(stream):
+            return quantize(x, transpose)
+    shape = x.shape
+    if len(shape) < 2:
+        raise ValueError("x: %d dimensions, at least 2 needed" % len(shape))
+    R, K = shape[-2:]
     if transpose:
         R, K = K, R
     if K % 32:
         raise ValueError("K = %d is not a multiple of 32" % K)
-    lead = x.shape[:-2]
-    with _on(stream):
-        codes = torch.empty((*lead, R, K // 2), dtype=torch.uint8, device=x.device)
-        scales = torch.empty((*lead, R, K // 32), dtype=torch.uint8, device=x.device)
-        flags = B.dtype_flag(x) | (B.MOE_TRANSPOSED if transpose else 0)
-        B.moe_mx_quantize(x, lead.numel(), R, K, flags, codes, scales, None)
+    lead, flags, dev = shape[:-2], B.dtype_flag(x), x.device
+    px, = B._args(B._current(), (x, 0, x.dtype, "x"))
+    codes = torch.empty((*lead, R, K // 2), dtype=torch.uint8, device=dev)
+    scales = torch.empty((*lead, R, K // 32), dtype=torch.uint8, device=dev)
+    B._check(B.load_library().moe_mx_quantize(
+        px, lead.numel(), R, K, flags | (B.MOE_TRANSPOSED if transpose else 0), codes.data_ptr(),
+        scales.data_ptr(), B._stream(None)))
     return MX(codes, scales)
 
 
 def dequantize(q: MX, dtype=torch.bfloat16, stream=None):
     """The values of ``q`` as bfloat16 or float32 (exact inside the type's range)."""
-    K = 2 * q.codes.shape[-1]
-    if q.scales.shape != (*q.codes.shape[:-1], K // 32) or K % 32:
+    if stream is not None:
+        with _on(stream):
+            return dequantize(q, dtype)
+    codes, scales = q
+    *lead, half = codes.shape
+    K = 2 * half
+    if scales.shape != (*lead, K // 32) or K % 32:
         raise ValueError("codes %s and scales %s do not belong together" %
-                         (tuple(q.codes.shape), tuple(q.scales.shape)))
-    with _on(stream):
-        out = torch.empty(q.shape, dtype=dtype, device=q.codes.device)
-        B.moe_mx_dequantize(q.codes, q.scales, out.numel() // K if K else 0, K, B.dtype_flag(out),
-                            out, None)
+                         (tuple(codes.shape), tuple(scales.shape)))
+    u8 = torch.uint8
+    pc, ps = B._args(B._current(), (codes, 0, u8, "codes"), (scales, 0, u8, "scales"))
+    out = torch.empty((*lead, K), dtype=dtype, device=codes.device)
+    if K:
+        B._check(B.load_library().moe_mx_dequantize(pc, ps, codes.numel() // half, K, B.dtype_flag(out),
+                                                    out.data_ptr(), B._stream(None)))
     return out
 
 
@@ -84,25 +96,29 @@ def product(x, w: MX, offsets, rows=None, w3: MX | None = None, act: str = "none
     ``x``: bfloat16 [T, K], or MX. ``w``, ``w3``: MX [E, N, K]. ``rows``: int32 [S], the
     row of x of each slot (expert_token_indices); None: slot s is row s. Returns ``out``
     [S, N] bfloat16; rows at or behind offsets[E] are not written."""
+    if stream is not None:
+        with _on(stream):
+            return product(x, w, offsets, rows, w3, act, out)
     if act not in ACT:
         raise ValueError("act %r is none of %s" % (act, sorted(ACT)))
     if (act == "swiglu") != (w3 is not None):
         raise ValueError("w3 goes with act='swiglu'")
     E, N, K = w.shape
-    if w3 is not None and w3.shape != w.shape:
-        raise ValueError("w3: %s, w is %s" % (tuple(w3.shape), tuple(w.shape)))
+    if w3 is not None and w3.shape != (E, N, K):
+        raise ValueError("w3: %s, w is %s" % (tuple(w3.shape), (E, N, K)))
     xc, xs = x if isinstance(x, MX) else (x, None)
     T, Kx = xc.shape
-    if (2 * Kx if xs is not None else Kx) != K:
-        raise ValueError("x: rows of %d, w sums over %d" % (2 * Kx if xs is not None else Kx, K))
+    if xs is not None:
+        Kx *= 2
+    if Kx != K:
+        raise ValueError("x: rows of %d, w sums over %d" % (Kx, K))
     S = T if rows is None else rows.numel()
-    with _on(stream):
-        if out is None:
-            out = torch.empty((S, N), dtype=torch.bfloat16, device=xc.device)
-        elif out.shape != (S, N):
-            raise ValueError("out: %s, expected %s" % (tuple(out.shape), (S, N)))
-        B.moe_mx_gemm(xc, xs, w.codes, w.scales, *(w3 or (None, None)), offsets, rows, T, S, K, N, E,
-                      ACT[act], out, None)
+    if out is None:
+        out = torch.empty((S, N), dtype=torch.bfloat16, device=xc.device)
+    elif out.shape != (S, N):
+        raise ValueError("out: %s, expected %s" % (tuple(out.shape), (S, N)))
+    B.moe_mx_gemm(xc, xs, w.codes, w.scales, *(w3 or (None, None)), offsets, rows, T, S, K, N, E,
+                  ACT[act], out, None)
     return out
 
 
