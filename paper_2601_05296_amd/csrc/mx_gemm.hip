@@ -14,6 +14,7 @@
 // The order of K inside a matrix instruction is free as long as both operands agree: the
 // layouts below give every lane whole blocks of 32 values, so that it needs one scale.
 #include <algorithm>
+#include <cmath>
 
 #include "gemm.hpp"
 #include "launch.hpp"
@@ -292,8 +293,8 @@ mx_stream(const Args a) {
 // BM x BN outputs of NB weights, WM x WN waves of 32 x 32 fragments. A slice is 64 values of
 // K with bfloat16 rows (128-byte rows of x, 32-byte rows of codes), 256 with 4-bit rows
 // (128-byte rows of either: whole lines take 40% fewer requests to L2 than slices of 128 do).
-// Each 64 values are two blocks; lane half h = L / 32 takes block h of them, one 16-byte LDS read of codes, which four 32x32x16 bfloat16 or one 32x32x64
-// scaled instruction use up. With bfloat16 rows instruction q takes values 8q .. 8q + 7 of
+// Each 64 values are two blocks; lane half h = L / 32 takes block h of them, one 16-byte LDS
+// read of codes, which four 32x32x16 bfloat16 or one 32x32x64 scaled instruction use up. With bfloat16 rows instruction q takes values 8q .. 8q + 7 of
 // both blocks, so x comes as the chunks at bytes 64 h + 16 q of its row.
 // Scales come for 512 values of K at a time, 16 bytes of each row as aligned dwords, four
 // lanes to a row, into one of three buffers: a piece of chunk c + 1 goes out with each slice
@@ -760,37 +761,58 @@ hipError_t tile(const MxArgs& m, const Args& a, hipStream_t st) {
     return go(std::false_type{});
 }
 
-// Times in us, bfloat16 rows, the alternatives on the same data.
+// Times in us, the alternatives on the same data.
 template <bool X4, int NB>
 hipError_t pick(const MxArgs& m, const Args& a, hipStream_t st) {
     // rows of an expert that has any, about, and workgroups of 64 columns
-    const double rows = (double)m.S / (double)std::min<int64_t>(m.S, m.E);
+    const int64_t active = std::min<int64_t>(m.S, m.E);
+    const double rows = (double)m.S / (double)active;
     const int64_t blocks = row_tiles(m.S, m.E, 16) * (m.N / 64);
     constexpr int BN = NB == 2 ? 128 : 256, NST = X4 ? 2 : 3;
     // Fewer workgroups than CUs, a row or so each (single tokens): 16 columns, and slices of
     // 1024 values, four waves deep. d = 14336 -> 4096, two experts: 13.9 against 22.8;
     // 2880 -> 2880 gated, four experts: 11.0, 12.2.
     if (m.S <= m.E && blocks < 256) return stream<SCfg<4, 16, 1, 4, 8, NB, X4, 2, 128>>(m, a, st);
-    if (rows <= 12) {
-        // A long K on few workgroups is bound by the steps of each one's loop: 16 waves, 512
-        // values a step. 14336 -> 4096, 8 experts, 32 tokens: 47.9, 56.2; the other way round
-        // with many workgroups (2880 -> 2880, 300 tokens, 128 experts): 150.8, 137.2.
-        if constexpr (NB == 1)
-            if (m.K >= 4096 && blocks <= 1024) return stream<SCfg<16, 64, 4, 4, 4, NB, X4, 2, 128>>(m, a, st);
-        return stream<SCfg<16, 64, 2, 2, 2, NB, X4, 2, 64>>(m, a, st);
+    // The largest tile that the rows fill and that still gives two thirds of the CUs one: its
+    // operands are used most often, but a workgroup takes as long on an idle chip as on a full
+    // one (K = 4096, bfloat16 rows, one weight, tiles of 256, 128, 64 and 32 rows: 79, 49, 38, 16).
+    // K -> N, rows of each of E experts; 256, 128, 64, 32 rows a tile:
+    //                                        bfloat16 rows, one weight    4-bit rows, gated
+    //   4096 -> 14336   8 x  32                   -  118  76.2  62.7          -   112   103  99.2
+    //                   8 x  64                 188  125  83.0  92.0        150   118   115   124
+    //                   8 x 128                 198  133   145    -         160   133   174     -
+    //                   8 x 512                 412  459   517    -         296   394     -     -
+    //   14336 -> 4096   8 x 128                 262  216   155    -         135   121   163     -
+    //                   8 x 256                 299  243   261    -         154   192     -     -
+    //   4096 -> 4096    2 x 128                79.0 49.3  38.8  17.5       28.7  22.2  16.3  15.8
+    //                   2 x 256                78.8 49.7  39.9  25.1       31.8  22.6  18.8  28.7
+    //                   2 x 1024               85.9 65.8  74.3  89.5       41.9  47.9  63.6  79.6
+    //   2880 -> 2880    4 x 512                59.6 40.9  45.6  52.8       36.0  43.0  48.7  62.6
+    auto fills = [&](int bm, int bn) {
+        return (double)active * std::ceil(rows / bm) * ((m.N + bn - 1) / bn) * 3.0 >= 2.0 * 256.0;
+    };
+    if (rows > 128 && fills(256, BN)) return tile<TCfg<256, BN, 2, 4, NB, X4, NST>>(m, a, st);
+    if (rows > 64 && fills(128, BN)) return tile<TCfg<128, BN, 2, 4, NB, X4, NST>>(m, a, st);
+    // With 4-bit rows half as many columns, twice the workgroups, where 64 rows: 4096 -> 14336,
+    // 8 x 48 rows 56.1, 58.8; 2048 -> 1408 gated, 64 x 48 rows 46.0, 49.3; bfloat16 rows, which
+    // four waves side by side convert once each: 98.3, 80.4; 70.4, 66.2.
+    constexpr int BN64 = X4 ? BN / 2 : BN;
+    if (rows > 32 && fills(64, BN64)) {
+        if constexpr (X4) return tile<TCfg<64, BN64, 2, 2, NB, X4, NST>>(m, a, st);
+        else return tile<TCfg<64, BN64, 1, 4, NB, X4, NST>>(m, a, st);
     }
     // 16 and 32 rows a tile: 9.4 rows an expert (2880 -> 2880) 276, 287; 24 rows (4096 ->
-    // 14336 gated) 144, 111
-    if (rows <= 24) {
+    // 14336 gated) 145, 105
+    if (rows > 12) {
         if constexpr (NB == 2) return stream<SCfg<32, 64, 2, 2, 2, NB, X4, 2, 64>>(m, a, st);
         else return stream<SCfg<32, 128, 4, 2, 2, NB, X4, 2, 64>>(m, a, st);
     }
-    if (rows <= 64) {
-        if constexpr (X4) return tile<TCfg<64, 128 / NB, 2, 2, NB, X4, NST>>(m, a, st);
-        else return tile<TCfg<64, BN, 1, 4, NB, X4, NST>>(m, a, st);
-    }
-    if (rows <= 128) return tile<TCfg<128, BN, 2, 4, NB, X4, NST>>(m, a, st);
-    return tile<TCfg<256, BN, 2, 4, NB, X4, NST>>(m, a, st);
+    // A long K on few workgroups is bound by the steps of each one's loop: 16 waves, 512
+    // values a step. 14336 -> 4096, 8 experts, 32 tokens: 47.9, 56.2; the other way round
+    // with many workgroups (2880 -> 2880, 300 tokens, 128 experts): 150.8, 137.2.
+    if constexpr (NB == 1)
+        if (m.K >= 4096 && blocks <= 1024) return stream<SCfg<16, 64, 4, 4, 4, NB, X4, 2, 128>>(m, a, st);
+    return stream<SCfg<16, 64, 2, 2, 2, NB, X4, 2, 64>>(m, a, st);
 }
 
 }  // namespace

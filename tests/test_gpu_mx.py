@@ -169,8 +169,9 @@ def _run(dev, ref, tol, spare=0):
     assert (got[ref.shape[0]:] == 77.0).all()
 
 
-# rows of each expert, chosen so that the mean picks each core: streams of 4, 16 and 32 rows,
-# tiles of 64, 128 and 256
+# rows of each expert, chosen so that the mean picks each core where N is WIDE: streams of 4,
+# 16 and 32 rows, tiles of 64, 128 and 256 (narrow products leave CUs idle: streams)
+WIDE = 11328   # 177 x 64
 LOADS = {
     "one": [0, 0, 1, 0], "same": [0, 7, 0, 0, 0, 0, 0, 0], "few": [3, 0, 17, 1, 0, 16, 0], "some": [40, 2, 0, 33, 16],
     "tile64": [64, 1, 0, 130, 33], "tile128": [129, 128, 3, 0, 200], "tile256": [256, 300, 0, 1, 700, 255],
@@ -192,15 +193,27 @@ def test_product_over_loads(load, act, x4):
 def test_product_loads_reach_every_core():
     names = {}
     for load, counts in LOADS.items():
-        dev, *_ = _case(counts, 50, 128, 64, "none", False, True)
+        dev, *_ = _case(counts, 50, 128, WIDE, "none", False, True)
         names[load] = launched(lambda: mx.product(**dev))
     assert [names[n] for n in LOADS] == [["mx_stream"]] * 4 + [["mx_tile"]] * 3
+
+
+@pytest.mark.parametrize("load", ["some", "tile64", "tile128", "tile256"])
+@pytest.mark.parametrize("act", ["none", "swiglu"])
+@pytest.mark.parametrize("x4", [False, True])
+def test_product_wide_loads(load, act, x4):
+    """Tiles, over depths of one slice, of slices cut short and of rows that are no whole slices."""
+    for K, gather in ((64, True), (320, False), (576, True), (1024, False)) + (() if act == "swiglu" else ((4160, True),)):
+        print(load, act, x4, K, gather, flush=True)
+        dev, ref, tol = _case(LOADS[load], 50, K, WIDE, act, x4, gather, seed=K, spare=3)
+        _run(dev, ref, tol, 3)
 
 
 @pytest.mark.parametrize("act", ["silu", "relu"])
 @pytest.mark.parametrize("load", ["few", "tile128"])
 def test_product_activations(load, act):
     _run(*_case(LOADS[load], 40, 256, 128, act, False, True, seed=9))
+    _run(*_case(LOADS[load], 40, 128, WIDE, act, True, True, seed=10))
 
 
 @pytest.mark.parametrize("K,N", [(64, 128), (128, 64), (192, 256), (1408, 2048), (2880, 2880), (4096, 192), (8192, 64)])
@@ -237,11 +250,11 @@ def test_product_many_experts(x4):
         _run(*_case(counts, 64, 64, 64, "none", x4, True, seed=E))
 
 
-@pytest.mark.parametrize("counts", [[9, 2], [90, 40]])
+@pytest.mark.parametrize("counts,N", [([9, 2], 64), ([90, 40], 64), ([90, 40, 70, 80], WIDE)])
 @pytest.mark.parametrize("x4", [False, True])
-def test_product_extreme_scales(counts, x4):
+def test_product_extreme_scales(counts, N, x4):
     """Scale bytes 0 and 254, and 255 (NaN) in one column of one weight and one row of x."""
-    K, N = 192, 64
+    K = 192
     dev, ref, tol = _case(counts, 20, K, N, "none", x4, False, seed=2)
     dev["w"].scales[0, 5] = 0
     dev["w"].scales[1, 6, 2] = 255
@@ -250,7 +263,7 @@ def test_product_extreme_scales(counts, x4):
         dev["x"].scales[1] = 255
     out = mx.product(**dev).double().cpu().numpy()
     nan = np.zeros_like(ref, bool)
-    nan[counts[0]:, 6] = True
+    nan[counts[0]:counts[0] + counts[1], 6] = True
     if x4:
         nan[1] = True
     assert np.array_equal(np.isnan(out), nan)
@@ -279,8 +292,8 @@ def test_product_extreme_scales(counts, x4):
 
 def test_product_row_of_x_with_nan_stays_alone():
     """A NaN or infinite row of x reaches its own slots only, also where its tile pads rows."""
-    for counts in ([6, 0, 3], [100, 45]):
-        dev, ref, tol = _case(counts, 10, 128, 64, "none", False, False, seed=4)
+    for counts, N in (([6, 0, 3], 64), ([100, 45], 64), ([100, 45, 70, 80], WIDE)):
+        dev, ref, tol = _case(counts, 10, 128, N, "none", False, False, seed=4)
         dev["x"][2, 7] = float("nan")
         dev["x"][counts[0], 1] = float("inf")
         out = mx.product(**dev).double().cpu().numpy()
@@ -290,8 +303,9 @@ def test_product_row_of_x_with_nan_stays_alone():
         assert (np.abs(out - ref)[~hit] <= tol[~hit]).all()
 
 
-def test_product_same_bits_again_in_a_graph_and_on_another_stream():
-    dev, ref, tol = _case([30, 0, 200, 7], 60, 256, 192, "swiglu", False, True, seed=6)
+@pytest.mark.parametrize("N", [192, WIDE])
+def test_product_same_bits_again_in_a_graph_and_on_another_stream(N):
+    dev, ref, tol = _case([30, 0, 200, 7], 60, 256, N, "swiglu", False, True, seed=6)
     want = mx.product(**dev)
     side = torch.cuda.Stream()
     side.wait_stream(torch.cuda.current_stream())
