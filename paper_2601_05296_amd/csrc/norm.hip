@@ -223,7 +223,7 @@ struct BwdArgs {
 // so a row takes one exchange between its waves instead of two. Column sums stay in
 // registers over all of a workgroup's rows; the workgroups' sums are added in
 // norm_bwd_sum, always in the same order.
-template <class S>
+template <class S, int KIND>
 __global__ void __launch_bounds__(S::THREADS)
 norm_bwd_kernel(const BwdArgs a) {
     using V = Vec<S::F32>;
@@ -235,8 +235,9 @@ norm_bwd_kernel(const BwdArgs a) {
     const int c0 = (wv % S::WPR) * 64 + (threadIdx.x & 63);
     const int nvec = a.d / EPV;
     const bool post = a.w_post != nullptr, pre = a.w_pre != nullptr;
-    const bool block = a.dy != nullptr, need_y = block && (post || a.kind != GATE_NONE);
-    const bool has_dr = a.dr != nullptr, full = a.kind == GATE_FULL;
+    const bool block = a.dy != nullptr, need_y = block && (post || KIND != GATE_NONE);
+    const bool has_dr = a.dr != nullptr;
+    constexpr bool full = KIND == GATE_FULL;
     const float inv_d = 1.0f / (float)a.d;
     auto vec = [&](const void* p, int64_t row, int i) {
         return static_cast<const uint4*>(p) + row * nvec + c0 + i * S::WPR * 64;
@@ -249,7 +250,7 @@ norm_bwd_kernel(const BwdArgs a) {
         if (!in(i)) continue;
         if (post) wpo[i] = *vec(a.w_post, 0, i);
         if (pre) wpr[i] = *vec(a.w_pre, 0, i);
-        if (a.kind == GATE_CHANNEL) gc[i] = *vec(a.gate, 0, i);
+        if (KIND == GATE_CHANNEL) gc[i] = *vec(a.gate, 0, i);
     }
     float awpr[NV][EPV] = {}, awpo[NV][EPV] = {}, agc[NV][EPV] = {};
     uint4 ldr[NV], ldn[NV], lr[NV], ly[NV];
@@ -267,13 +268,17 @@ norm_bwd_kernel(const BwdArgs a) {
         }
         if (post) rpo = a.rstd_post[t];
         if (pre) rpr = a.rstd_pre[t];
-        if (a.kind == GATE_TOKEN) gt = V::one(a.gate, t);
+        if (KIND == GATE_TOKEN) gt = V::one(a.gate, t);
     };
     const int64_t step = (int64_t)gridDim.x * S::RPB;
-    load((int64_t)blockIdx.x * S::RPB + grp);
+    // four vectors of everything twice would not fit the registers (8192 float32, channel gate:
+    // 8192 rows: 474 us with spills, 345 without a row ahead)
+    constexpr bool AHEAD = NV < 4;
+    if (AHEAD) load((int64_t)blockIdx.x * S::RPB + grp);
     for (int64_t t0 = (int64_t)blockIdx.x * S::RPB; t0 < a.T; t0 += step) {
         const int64_t t = t0 + grp;
         const bool row = t < a.T;
+        if (!AHEAD) load(t);
         uint4 cdr[NV], cdn[NV], cr[NV], cy[NV], cg[NV];
         const float rp = rpr, ro = rpo, gtok = gt;
 #pragma unroll
@@ -281,9 +286,9 @@ norm_bwd_kernel(const BwdArgs a) {
             cdr[i] = ldr[i]; cdn[i] = ldn[i]; cr[i] = lr[i]; cy[i] = ly[i];
             cg[i] = full && in(i) && row ? *vec(a.gate, t, i) : gc[i];
         }
-        load(t + step);
+        if (AHEAD) load(t + step);
         auto gate = [&](int i, float (&g)[EPV]) {
-            if (a.kind == GATE_CHANNEL || full) V::get(cg[i], g);
+            if (KIND == GATE_CHANNEL || full) V::get(cg[i], g);
             else
 #pragma unroll
                 for (int e = 0; e < EPV; ++e) g[e] = gtok;   // 1 without a gate
@@ -302,7 +307,7 @@ norm_bwd_kernel(const BwdArgs a) {
                     const float u = fmaf(rp, wdn, vdr[e]);
                     const float pn = post ? wo[e] * (vy[e] * ro) : vy[e];   // p
                     s[0] = fmaf(wdn, rhat, s[0]);
-                    const float q = a.kind == GATE_TOKEN ? pn : g[e] * pn;
+                    const float q = KIND == GATE_TOKEN ? pn : g[e] * pn;
                     s[1] = fmaf(q, u, s[1]);
                     s[2] = fmaf(q, rhat, s[2]);
                 }
@@ -312,8 +317,8 @@ norm_bwd_kernel(const BwdArgs a) {
         const float m = s[0] * inv_d;
         // sum(p G) for a token's gate, which may be zero and comes in afterwards, else sum(gate p G)
         const float pG = s[1] - rp * m * s[2];
-        const float m2 = (a.kind == GATE_TOKEN ? gtok * pG : pG) * inv_d;
-        if (a.kind == GATE_TOKEN && c0 == 0) static_cast<float*>(a.dgate)[t] = pG;
+        const float m2 = (KIND == GATE_TOKEN ? gtok * pG : pG) * inv_d;
+        if (KIND == GATE_TOKEN && c0 == 0) static_cast<float*>(a.dgate)[t] = pG;
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
             if (!in(i)) continue;
@@ -347,19 +352,35 @@ norm_bwd_kernel(const BwdArgs a) {
             if (full) *const_cast<uint4*>(vec(a.dgate, t, i)) = V::put(dg);
         }
     }
-    // this row group's column sums, four floats a store
-    float* part = a.part + ((int64_t)blockIdx.x * S::RPB + grp) * 3 * a.d;
+    // the workgroup's column sums, its row groups' added in order
+    float* part = a.part + (int64_t)blockIdx.x * 3 * a.d;
+    __shared__ f32x4 cols[S::RPB > 1 ? S::RPB : 1][S::RPB > 1 ? 64 * NV * EPV / 4 : 1];
+    auto put = [&](const float (&acc)[NV][EPV], float* out) __attribute__((always_inline)) {
+        if constexpr (S::RPB > 1) __syncthreads();
 #pragma unroll
-    for (int i = 0; i < NV; ++i) {
-        if (!in(i)) continue;
-        const int c = (c0 + i * S::WPR * 64) * EPV;
+        for (int i = 0; i < NV; ++i) {
+            if (!in(i)) continue;
+            const int c = (c0 + i * S::WPR * 64) * EPV;
 #pragma unroll
-        for (int e = 0; e < EPV; e += 4) {
-            if (pre) *reinterpret_cast<f32x4*>(part + c + e) = f32x4{awpr[i][e], awpr[i][e + 1], awpr[i][e + 2], awpr[i][e + 3]};
-            if (post) *reinterpret_cast<f32x4*>(part + a.d + c + e) = f32x4{awpo[i][e], awpo[i][e + 1], awpo[i][e + 2], awpo[i][e + 3]};
-            if (a.kind == GATE_CHANNEL) *reinterpret_cast<f32x4*>(part + 2 * a.d + c + e) = f32x4{agc[i][e], agc[i][e + 1], agc[i][e + 2], agc[i][e + 3]};
+            for (int e = 0; e < EPV; e += 4) {
+                const f32x4 v{acc[i][e], acc[i][e + 1], acc[i][e + 2], acc[i][e + 3]};
+                if constexpr (S::RPB > 1) cols[grp][(c + e) / 4] = v;
+                else *reinterpret_cast<f32x4*>(out + c + e) = v;
+            }
         }
-    }
+        if constexpr (S::RPB > 1) {
+            __syncthreads();
+            for (int c = threadIdx.x; c < a.d / 4; c += S::THREADS) {
+                f32x4 v = cols[0][c];
+#pragma unroll
+                for (int g = 1; g < S::RPB; ++g) v += cols[g][c];
+                *reinterpret_cast<f32x4*>(out + c * 4) = v;
+            }
+        }
+    };
+    if (pre) put(awpr, part);
+    if (post) put(awpo, part + a.d);
+    if constexpr (KIND == GATE_CHANNEL) put(agc, part + 2 * a.d);
 }
 
 // out[c] = sum over the P partial sums of column c: 32 lanes of four columns by 32
@@ -405,17 +426,18 @@ void with_shape(int d, F&& f) {
 }
 
 // Workgroups of the backward: 8 waves a CU hold enough loads in flight, and each more
-// would write another 3 d partial sums.
+// would write another 3 d partial sums (16383 x 4096, channel gate: 8 waves 163 us, 12 178, 16
+// 175; 4 are too few for short rows, 60000 x 512: 73 and 105).
 template <class S>
 int bwd_blocks(int64_t T) {
     constexpr int W = S::THREADS / 64;
     return row_blocks(T, S::RPB, W >= 8 ? 256 : 256 * 8 / W);
 }
 
-// partial sums of a column
+// partial sums of a column: one a workgroup
 int bwd_parts(int64_t T, int d, bool f32) {
     int P = 0;
-    auto count = [&](auto s) { P = bwd_blocks<decltype(s)>(T) * decltype(s)::RPB; };
+    auto count = [&](auto s) { P = bwd_blocks<decltype(s)>(T); };
     if (f32) with_shape<true>(d, count);
     else with_shape<false>(d, count);
     return P;
@@ -435,7 +457,9 @@ template <bool F32>
 void launch_bwd(const BwdArgs& a, hipStream_t st) {
     with_shape<F32>(a.d, [&](auto s) {
         using S = decltype(s);
-        hipLaunchKernelGGL((norm_bwd_kernel<S>), dim3(bwd_blocks<S>(a.T)), dim3(S::THREADS), 0, st, a);
+        const auto kernel = a.kind == GATE_NONE ? &norm_bwd_kernel<S, GATE_NONE> : a.kind == GATE_CHANNEL ? &norm_bwd_kernel<S, GATE_CHANNEL>
+                          : a.kind == GATE_TOKEN ? &norm_bwd_kernel<S, GATE_TOKEN> : &norm_bwd_kernel<S, GATE_FULL>;
+        hipLaunchKernelGGL(kernel, dim3(bwd_blocks<S>(a.T)), dim3(S::THREADS), 0, st, a);
     });
     probe::mark("norm_bwd", st);
 }
