@@ -812,6 +812,19 @@ hipError_t pick(const MxArgs& m, const Args& a, hipStream_t st) {
     // with many workgroups (2880 -> 2880, 300 tokens, 128 experts): 150.8, 137.2.
     if constexpr (NB == 1)
         if (m.K >= 4096 && blocks <= 1024) return stream<SCfg<16, 64, 4, 4, 4, NB, X4, 2, 128>>(m, a, st);
+    // bfloat16 rows cost LDS and L2 as much as the weights of 64 columns do: 192 columns, two
+    // workgroups a CU, where they fill their rounds over the chip as well as 64 columns, four
+    // workgroups a CU, do. 9 rows an expert, 128 x 2880 -> 2880 (3.75 rounds of 4; 5.6 of 6) 128.5,
+    // 136.3; 64 x 2048 -> 1408 (1 of 1; 1.4 of 2) 20.2, 24.3; 64 x 1408 -> 2048 (1.4 of 2; 2 of 2)
+    // 30.3, 26.0. With 4-bit rows no faster: 124.1, 124.5; 19.6, 20.1; 29.5, 25.8.
+    if constexpr (NB == 1 && !X4) {
+        auto rounds = [&](int bn, int wgs) {
+            return (double)active * std::ceil(rows / 16) * ((m.N + bn - 1) / bn) / wgs;
+        };
+        const double wide = rounds(192, 512), narrow = rounds(64, 1024);
+        if (wide >= 1 && wide / std::ceil(wide) >= narrow / std::ceil(narrow))
+            return stream<SCfg<16, 192, 4, 2, 2, NB, X4, 2, 64>>(m, a, st);
+    }
     return stream<SCfg<16, 64, 2, 2, 2, NB, X4, 2, 64>>(m, a, st);
 }
 

@@ -250,6 +250,15 @@ def test_product_many_experts(x4):
         _run(*_case(counts, 64, 64, 64, "none", x4, True, seed=E))
 
 
+@pytest.mark.parametrize("x4", [False, True])
+def test_product_many_experts_whole_rounds(x4):
+    """Workgroups enough for whole rounds over the chip, the widest tiles ending behind N."""
+    counts = np.random.default_rng(4).poisson(6, 256).tolist()
+    for K, N in ((64, 640), (320, 640), (1088, 320)):
+        print(K, N, flush=True)
+        _run(*_case(counts, 64, K, N, "none", x4, True, seed=K))
+
+
 @pytest.mark.parametrize("counts,N", [([9, 2], 64), ([90, 40], 64), ([90, 40, 70, 80], WIDE)])
 @pytest.mark.parametrize("x4", [False, True])
 def test_product_extreme_scales(counts, N, x4):
