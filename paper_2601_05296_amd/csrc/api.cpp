@@ -648,7 +648,8 @@ int moe_mx_quantize(const void* src, int64_t batch, int64_t R, int K, unsigned f
     if (flags & MOE_TRANSPOSED) {
         if (R % 2) return fail(MOE_ERR_UNSUPPORTED, "%s: R = %lld is odd (MOE_TRANSPOSED)", fn, (long long)R);
         if (batch > 65535) return fail(MOE_ERR_UNSUPPORTED, "%s: batch = %lld > 65535 (MOE_TRANSPOSED)", fn, (long long)batch);
-        if (K > 65535 * 256) return fail(MOE_ERR_UNSUPPORTED, "%s: K = %d > 65535 * 256 (MOE_TRANSPOSED)", fn, K);
+        if (R >= (1 << 29)) return fail(MOE_ERR_UNSUPPORTED, "%s: R = %lld, 2^29 or more (MOE_TRANSPOSED)", fn, (long long)R);
+        if (K > (1 << 24)) return fail(MOE_ERR_UNSUPPORTED, "%s: K = %d > 2^24 (MOE_TRANSPOSED)", fn, K);
     }
     if (batch == 0 || R == 0) return MOE_OK;
     REQUIRE_PTR(src); REQUIRE_PTR(codes); REQUIRE_PTR(scales);

@@ -138,6 +138,8 @@ def test_mx_refusals():
     assert quant(flags=B.MOE_RENORM) == INV and quant(src=None) == INV and quant(codes=FAKE + 4) == INV
     assert quant(rows=3, flags=B.MOE_TRANSPOSED) == UNS
     assert quant(batch=65536, rows=2, flags=B.MOE_TRANSPOSED) == UNS
+    assert quant(rows=1 << 29, K=32, flags=B.MOE_TRANSPOSED) == UNS
+    assert quant(rows=2, K=(1 << 24) + 32, flags=B.MOE_TRANSPOSED) == UNS
     assert quant(batch=1 << 20, rows=1 << 20) == UNS
     assert quant(rows=0, src=None) == B.MOE_OK and quant(batch=0, src=None) == B.MOE_OK
     deq = lib.moe_mx_dequantize
