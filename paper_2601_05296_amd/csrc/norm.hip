@@ -40,10 +40,13 @@ struct Vec {
         else
             return pack8(o);
     }
-    static __device__ __forceinline__ float one(const void* p, int64_t i) {
-        if constexpr (F32) return static_cast<const float*>(p)[i];
-        else return bf2f(static_cast<const bf16_t*>(p)[i]);
+    // one element as it lies in memory, and as a float: converting it where it is loaded would
+    // wait for it, and with it for all loads of a row ahead
+    static __device__ __forceinline__ uint32_t raw(const void* p, int64_t i) {
+        if constexpr (F32) return static_cast<const uint32_t*>(p)[i];
+        else return static_cast<const uint16_t*>(p)[i];
     }
+    static __device__ __forceinline__ float one(uint32_t raw) { return __uint_as_float(F32 ? raw : raw << 16); }
 };
 
 // A row is held by WPR waves, NV vectors a lane: lane l of the row's wave w holds
@@ -93,10 +96,13 @@ struct FwdArgs {
     int d, kind;
 };
 
+// Bound by HBM: res, y in, r, n out, 5.2 to 5.4 TB/s (32768 x 4096 bfloat16 197 to 206 us, a
+// copy's rate). The gate's kind is a template argument: as one of the launch it took 16383 x
+// 2880 from 70-77 us to 85-99.
 // Workgroups walk over the rows with the weights in registers and the next row's loads
 // issued before the present row's sums. r may take the place of res (or y), and n that
 // of y: a row's stores follow its loads, and no other workgroup touches the row.
-template <class S>
+template <class S, int KIND>
 __global__ void __launch_bounds__(S::THREADS)
 norm_fwd_kernel(const FwdArgs a) {
     using V = Vec<S::F32>;
@@ -107,7 +113,7 @@ norm_fwd_kernel(const FwdArgs a) {
     const int c0 = (wv % S::WPR) * 64 + (threadIdx.x & 63);
     const int nvec = a.d / EPV;
     const bool block = a.y != nullptr, post = a.w_post != nullptr, pre = a.w_pre != nullptr;
-    const bool full = a.kind == GATE_FULL;
+    constexpr bool full = KIND == GATE_FULL;
     const float inv_d = 1.0f / (float)a.d;
     auto vec = [&](const void* p, int64_t row, int i) {
         return static_cast<const uint4*>(p) + row * nvec + c0 + i * S::WPR * 64;
@@ -119,10 +125,10 @@ norm_fwd_kernel(const FwdArgs a) {
         if (!in(i)) continue;
         if (post) wpo[i] = *vec(a.w_post, 0, i);
         if (pre) wpr[i] = *vec(a.w_pre, 0, i);
-        if (a.kind == GATE_CHANNEL) gc[i] = *vec(a.gate, 0, i);
+        if (KIND == GATE_CHANNEL) gc[i] = *vec(a.gate, 0, i);
     }
     uint4 y[NV], x[NV], g[NV];
-    float gt = 1.0f;
+    uint32_t gt = 0;
     auto load = [&](int64_t t) {
         if (t >= a.T) return;
 #pragma unroll
@@ -132,7 +138,7 @@ norm_fwd_kernel(const FwdArgs a) {
             if (block) y[i] = *vec(a.y, t, i);
             if (full) g[i] = *vec(a.gate, t, i);
         }
-        if (a.kind == GATE_TOKEN) gt = V::one(a.gate, t);
+        if (KIND == GATE_TOKEN) gt = V::raw(a.gate, t);
     };
     const int64_t step = (int64_t)gridDim.x * S::RPB;
     load((int64_t)blockIdx.x * S::RPB + grp);
@@ -155,7 +161,7 @@ norm_fwd_kernel(const FwdArgs a) {
         if (full)
 #pragma unroll
             for (int i = 0; i < NV; ++i) V::get(g[i], gv[i]);
-        const float gtok = gt;
+        const float gtok = V::one(gt);
         load(t + step);
         if (post) {
 #pragma unroll
@@ -176,10 +182,10 @@ norm_fwd_kernel(const FwdArgs a) {
         if (block) {
 #pragma unroll
             for (int i = 0; i < NV; ++i) {
-                if (a.kind == GATE_CHANNEL) V::get(gc[i], gv[i]);
+                if (KIND == GATE_CHANNEL) V::get(gc[i], gv[i]);
 #pragma unroll
                 for (int e = 0; e < EPV; ++e) {
-                    const float ge = a.kind == GATE_NONE ? 1.0f : a.kind == GATE_TOKEN ? gtok : gv[i][e];
+                    const float ge = KIND == GATE_NONE ? 1.0f : KIND == GATE_TOKEN ? gtok : gv[i][e];
                     r[i][e] = fmaf(a.res_scale, r[i][e], ge * p[i][e]);
                 }
                 if (in(i) && row) *const_cast<uint4*>(vec(a.r, t, i)) = V::put(r[i]);
@@ -223,6 +229,10 @@ struct BwdArgs {
 // so a row takes one exchange between its waves instead of two. Column sums stay in
 // registers over all of a workgroup's rows; the workgroups' sums are added in
 // norm_bwd_sum, always in the same order.
+// Bound by HBM: dr, dn, y, r in, dres, dy out, 5.5 TB/s (16383 x 4096 bfloat16 147 us, 5 of
+// them the sums' launch; a copy reaches 4.7 to 5.2, half of its bytes being writes, here a
+// third). The gate's kind is a template argument: one kernel for all kinds spilled (184 us). Row
+// groups that share a workgroup add their sums in LDS first: 60000 x 512 84 to 73 us.
 template <class S, int KIND>
 __global__ void __launch_bounds__(S::THREADS)
 norm_bwd_kernel(const BwdArgs a) {
@@ -253,10 +263,11 @@ norm_bwd_kernel(const BwdArgs a) {
         if (KIND == GATE_CHANNEL) gc[i] = *vec(a.gate, 0, i);
     }
     float awpr[NV][EPV] = {}, awpo[NV][EPV] = {}, agc[NV][EPV] = {};
-    uint4 ldr[NV], ldn[NV], lr[NV], ly[NV];
-    float rpo = 1.f, rpr = 0.f, gt = 1.f;
+    uint4 ldr[NV], ldn[NV], lr[NV], ly[NV], lg[NV];
+    float rpo = 1.f, rpr = 0.f;
+    uint32_t gt = 0;
 #pragma unroll
-    for (int i = 0; i < NV; ++i) ldr[i] = ldn[i] = lr[i] = ly[i] = zero16();
+    for (int i = 0; i < NV; ++i) ldr[i] = ldn[i] = lr[i] = ly[i] = lg[i] = zero16();
     auto load = [&](int64_t t) {
         if (t >= a.T) return;
 #pragma unroll
@@ -265,10 +276,11 @@ norm_bwd_kernel(const BwdArgs a) {
             if (has_dr) ldr[i] = *vec(a.dr, t, i);
             if (pre) { ldn[i] = *vec(a.dn, t, i); lr[i] = *vec(a.r, t, i); }
             if (need_y) ly[i] = *vec(a.y, t, i);
+            if (full) lg[i] = *vec(a.gate, t, i);
         }
         if (post) rpo = a.rstd_post[t];
         if (pre) rpr = a.rstd_pre[t];
-        if (KIND == GATE_TOKEN) gt = V::one(a.gate, t);
+        if (KIND == GATE_TOKEN) gt = V::raw(a.gate, t);
     };
     const int64_t step = (int64_t)gridDim.x * S::RPB;
     // four vectors of everything twice would not fit the registers (8192 float32, channel gate:
@@ -280,11 +292,11 @@ norm_bwd_kernel(const BwdArgs a) {
         const bool row = t < a.T;
         if (!AHEAD) load(t);
         uint4 cdr[NV], cdn[NV], cr[NV], cy[NV], cg[NV];
-        const float rp = rpr, ro = rpo, gtok = gt;
+        const float rp = rpr, ro = rpo, gtok = KIND == GATE_TOKEN ? V::one(gt) : 1.f;
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
             cdr[i] = ldr[i]; cdn[i] = ldn[i]; cr[i] = lr[i]; cy[i] = ly[i];
-            cg[i] = full && in(i) && row ? *vec(a.gate, t, i) : gc[i];
+            cg[i] = full ? lg[i] : gc[i];
         }
         if (AHEAD) load(t + step);
         auto gate = [&](int i, float (&g)[EPV]) {
@@ -354,7 +366,7 @@ norm_bwd_kernel(const BwdArgs a) {
     }
     // the workgroup's column sums, its row groups' added in order
     float* part = a.part + (int64_t)blockIdx.x * 3 * a.d;
-    __shared__ f32x4 cols[S::RPB > 1 ? S::RPB : 1][S::RPB > 1 ? 64 * NV * EPV / 4 : 1];
+    __shared__ f32x4 cols[S::RPB > 1 ? S::RPB : 1][S::RPB > 1 ? S::WPR * 64 * NV * EPV / 4 : 1];
     auto put = [&](const float (&acc)[NV][EPV], float* out) __attribute__((always_inline)) {
         if constexpr (S::RPB > 1) __syncthreads();
 #pragma unroll
@@ -405,7 +417,8 @@ norm_bwd_sum(const float* __restrict__ part, int P, int d, float* dw_pre, float*
     *reinterpret_cast<f32x4*>(out + c) = v;
 }
 
-// Rows are spread over the fewest workgroups that need the same number of passes.
+// Rows are spread over the fewest workgroups that need the same number of passes. The forward
+// allows 32 waves a CU (16383 x 4096, no gate: 102 us; 16 waves 119, 8 110).
 int row_blocks(int64_t T, int rpb, int most) {
     const int64_t n = (T + rpb - 1) / rpb;
     if (n <= most) return (int)n;
@@ -413,49 +426,61 @@ int row_blocks(int64_t T, int rpb, int most) {
     return (int)((n + passes - 1) / passes);
 }
 
-// f(Shape) for rows of d elements: waves a row and vectors a lane as few as hold it
-template <bool F32, class F>
+// f(Shape) for rows of d elements. The backward holds three column sums a lane beside its
+// rows, so it takes one vector a lane up to 512 of them, and six waves where those hold the
+// row; the forward fewer waves of two. us, forward and backward, bfloat16, channel gate:
+//   16383 x 4096   4 waves of 2: 99, 163   8 of 1: 107, 147
+//   16383 x 2880   4 waves of 2: 77, 117   6 of 1:  -, 109   8 of 1: 83, 121
+//   60000 x 1024   1 wave of 2:  97, 148   2 of 1: 97, 137
+//   8192 x 8192    8 waves of 2: 96, 159   16 of 1: 98, 665 (spills)
+template <bool F32, bool BWD, class F>
 void with_shape(int d, F&& f) {
     const int nvec = d / Vec<F32>::N;
     if (nvec <= 64) f(Shape<F32, 1, 1, 4>{});
+    else if (BWD && nvec <= 128) f(Shape<F32, 2, 1, 2>{});
     else if (nvec <= 128) f(Shape<F32, 1, 2, 4>{});
     else if (nvec <= 256) f(Shape<F32, 4, 1, 1>{});
+    else if (BWD && nvec <= 384) f(Shape<F32, 6, 1, 1>{});
+    else if (BWD && nvec <= 512) f(Shape<F32, 8, 1, 1>{});
     else if (nvec <= 512) f(Shape<F32, 4, 2, 1>{});
     else if (nvec <= 1024) f(Shape<F32, 8, 2, 1>{});
     else if constexpr (F32) f(Shape<F32, 8, 4, 1>{});   // d <= 8192
 }
 
-// Workgroups of the backward: 8 waves a CU hold enough loads in flight, and each more
-// would write another 3 d partial sums (16383 x 4096, channel gate: 8 waves 163 us, 12 178, 16
-// 175; 4 are too few for short rows, 60000 x 512: 73 and 105).
+// Workgroups of the backward: 8 waves (or one workgroup of 6) a CU hold enough loads in flight,
+// and each more would write another 3 d partial sums. 16383 x 4096 in workgroups of 4 waves,
+// channel gate: 8 waves a CU 163 us, 12 178, 16 175; 16383 x 2880 in workgroups of 6: one a CU
+// 109, two 116; 4 waves are too few, 60000 x 512: 8 73, 4 105.
 template <class S>
 int bwd_blocks(int64_t T) {
     constexpr int W = S::THREADS / 64;
-    return row_blocks(T, S::RPB, W >= 8 ? 256 : 256 * 8 / W);
+    return row_blocks(T, S::RPB, 256 * (8 / W));   // the same on every CU
 }
 
 // partial sums of a column: one a workgroup
 int bwd_parts(int64_t T, int d, bool f32) {
     int P = 0;
     auto count = [&](auto s) { P = bwd_blocks<decltype(s)>(T); };
-    if (f32) with_shape<true>(d, count);
-    else with_shape<false>(d, count);
+    if (f32) with_shape<true, true>(d, count);
+    else with_shape<false, true>(d, count);
     return P;
 }
 
 template <bool F32>
 void launch_fwd(const FwdArgs& a, hipStream_t st) {
-    with_shape<F32>(a.d, [&](auto s) {
+    with_shape<F32, false>(a.d, [&](auto s) {
         using S = decltype(s);
         const int grid = row_blocks(a.T, S::RPB, 256 * 32 / (S::THREADS / 64));
-        hipLaunchKernelGGL((norm_fwd_kernel<S>), dim3(grid), dim3(S::THREADS), 0, st, a);
+        const auto kernel = a.kind == GATE_NONE ? &norm_fwd_kernel<S, GATE_NONE> : a.kind == GATE_CHANNEL ? &norm_fwd_kernel<S, GATE_CHANNEL>
+                          : a.kind == GATE_TOKEN ? &norm_fwd_kernel<S, GATE_TOKEN> : &norm_fwd_kernel<S, GATE_FULL>;
+        hipLaunchKernelGGL(kernel, dim3(grid), dim3(S::THREADS), 0, st, a);
     });
     probe::mark("norm_fwd", st);
 }
 
 template <bool F32>
 void launch_bwd(const BwdArgs& a, hipStream_t st) {
-    with_shape<F32>(a.d, [&](auto s) {
+    with_shape<F32, true>(a.d, [&](auto s) {
         using S = decltype(s);
         const auto kernel = a.kind == GATE_NONE ? &norm_bwd_kernel<S, GATE_NONE> : a.kind == GATE_CHANNEL ? &norm_bwd_kernel<S, GATE_CHANNEL>
                           : a.kind == GATE_TOKEN ? &norm_bwd_kernel<S, GATE_TOKEN> : &norm_bwd_kernel<S, GATE_FULL>;

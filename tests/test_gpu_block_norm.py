@@ -87,12 +87,12 @@ def test_norms_over_widths(T, d, dtype):
 @pytest.mark.parametrize("post,pre", [(True, True), (True, False), (False, True), (False, False)])
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 def test_norms_over_variants(gate, post, pre, dtype):
-    for T, d in ((37, 256), (6, 2304)):
+    for T, d in ((37, 256), (6, 2304), (21, 1024), (300, 3080)):
         print(T, d, flush=True)
         _check(_make(T, d, dtype, gate, post, pre, 3), dtype, 1.0, T, d)
 
 
-@pytest.mark.parametrize("T,d", [(9001, 64), (6007, 1536), (3001, 4096)])
+@pytest.mark.parametrize("T,d", [(9001, 64), (6007, 1536), (3001, 4096), (5003, 1000), (2999, 3048), (1500, 8000)])
 def test_norms_many_rows_a_workgroup(T, d):
     print(T, d, flush=True)
     _check(_make(T, d, "bf16", "token", True, True, 1), "bf16", 0.5, T, d)
