@@ -8,6 +8,9 @@
 // one convert and one fused multiply-add per element take a quarter of the time that
 // reading the element does), so the sum of several devices' or calls' results is exact
 // enough to add up. Partial sums are added in one fixed order: no atomics.
+// 554 million float32 values: the norm 365 us, 6.1 TB/s, the highest rate reached for reading;
+// scaling them into other tensors 890 us, 5.0 TB/s, a copy's. (Scaling them from the last
+// piece to the first, which a cache might still hold: no faster.)
 #include "common.hpp"
 #include "launch.hpp"
 #include "probe.hpp"

@@ -38,7 +38,8 @@ __device__ __forceinline__ uint32_t top8(const float (&v)[8]) {
 }
 
 // Four lanes a block, eight values a lane: each wave reads and writes consecutive bytes.
-// UN groups a thread, all loads ahead.
+// UN groups a thread, all loads ahead. 64 x 2048 x 1408 bfloat16 77 us, 6.1 TB/s (four fifths
+// of the bytes are reads); float32 153, 5.5.
 template <bool F32, int UN>
 __global__ void __launch_bounds__(QT)
 mx_quantize_rows(const void* __restrict__ src, int64_t groups, uint32_t* __restrict__ codes,
@@ -129,7 +130,8 @@ mx_quantize_transposed(const void* __restrict__ src_, int64_t R, int K, uint8_t*
     }
 }
 
-// 16 bytes of values a lane, UN times: 8 or, in float32, 4 codes. (Eight float32 values, two
+// 16 bytes of values a lane, UN times: 8 or, in float32, 4 codes. 64 x 2048 x 1408 to bfloat16
+// 81 us, 5.8 TB/s, to float32 156, 5.3, mostly writes either way. (Eight float32 values, two
 // stores a lane 32 bytes apart from its neighbours': 4.0 TB/s, half lines a store.)
 template <bool F32, int UN>
 __global__ void __launch_bounds__(QT)

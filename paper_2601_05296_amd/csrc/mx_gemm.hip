@@ -290,6 +290,12 @@ mx_stream(const Args a) {
 }
 
 // ---- tile core --------------------------------------------------------------------------
+// Measured: 4-bit rows 4096 -> 14336 gated, eight experts, 3554 slots (444 rows each in tiles
+// of 256) 304 us, 2.75 PFLOP/s; 16384 slots 2.97; one 8192 x 8192 x 8192 product 3.6, where a
+// loop of the scaled instruction alone reaches 4.5. bfloat16 rows 2048 -> 1408 gated, 64 experts,
+// 98304 slots 975 to 1030 us, 1.1 to 1.16 PFLOP/s; 8192 x 8192 x 8192 1.28. About 12 (8) us of
+// a tile's time, its first copies and its results, run beside no matrix instruction: one
+// workgroup a CU.
 // BM x BN outputs of NB weights, WM x WN waves of 32 x 32 fragments. A slice is 64 values of
 // K with bfloat16 rows (128-byte rows of x, 32-byte rows of codes), 256 with 4-bit rows
 // (128-byte rows of either: whole lines take 40% fewer requests to L2 than slices of 128 do).
