@@ -434,22 +434,46 @@ mx_tile(const Args a) {
         dma4(p + min(c * 16, last), dst + (wv * C::NCS + i) * 256);
     };
     int sbuf = 1;   // buffer of the chunk after the one that the slices being issued are in
-    // copy u of this wave's C::PER of slice s, slices in order (4-bit rows: of slice 0, which K
-    // may cut short: chunk 0 stands in for those behind K, which are not used)
+    // Before the first copies of slice s of x's places [x0, x1) and, with W, of the weights: where
+    // K cuts the slice short, chunk 0 stands in for the chunks behind K, which are not used; where
+    // there is no such slice, the last one does. (4-bit rows; with bfloat16 ones slices are whole
+    // and none is copied that does not exist.)
+    auto edge = [&](int s, int x0, int x1, bool W) __attribute__((always_inline)) {
+        const int left = nkb - s * (C::KS / 32);
+        if (left >= C::KS / 32) return;
+        int r, l = lane;
+        asm volatile("" : "+v"(l));   // or the places below would be held in registers all along
+#pragma unroll
+        for (int i = 0; i < C::NCX; ++i) {
+            if (i < x0 || i >= x1) continue;
+            int c;
+            PX::at((wv + i * C::NW) * 64 + l, r, c);
+            px[i] -= left <= 0 ? C::XROW : c >= left ? c * 16 : 0;
+        }
+        if (!W) return;
+        if (left <= 0)
+#pragma unroll
+            for (int b = 0; b < C::NB; ++b) bw[b] -= C::WROW;
+        else
+#pragma unroll
+            for (int i = 0; i < C::NCW; ++i) {
+                int c;
+                PW::at((wv + i * C::NW) * 64 + l, r, c);
+                ow[i] -= c >= left ? c * 16 : 0;
+            }
+    };
+    // copy u of this wave's C::PER of slice s, slices in order
     auto issue = [&](int s, uint32_t dst, int u) __attribute__((always_inline)) {
-        int r;
         if (u < C::NCP) {
             copy_scales((s % C::SPC * C::NCP + u) * C::NCS / (C::SPC * C::NCP), s / C::SPC + 1, sbase + sbuf * C::S_BYTES);
             if (u == C::NCP - 1 && (s + 1) % C::SPC == 0) sbuf = sbuf == 2 ? 0 : sbuf + 1;
         } else if (u < C::NCP + C::NCX) {
             const int i = u - C::NCP;
-            const int c = chunk_x(i, r);
-            dma16(px[i] - (C::X4 && c >= nkb ? c * 16 : 0), dst + (wv + i * C::NW) * 1024);
+            dma16(px[i], dst + (wv + i * C::NW) * 1024);
             px[i] += C::XROW;
         } else {
             const int i = u - C::NCP - C::NCX;
-            const int c = chunk_w(i, r);
-            dma16_at(weight(i), ow[i] - (C::X4 && c >= nkb ? c * 16 : 0), dst + C::X_BYTES + (wv + i * C::NW) * 1024);
+            dma16_at(weight(i), ow[i], dst + C::X_BYTES + (wv + i * C::NW) * 1024);
             if (u == C::PER - 1)
 #pragma unroll
                 for (int b = 0; b < C::NB; ++b) bw[b] += C::WROW;
@@ -468,6 +492,7 @@ mx_tile(const Args a) {
     __builtin_amdgcn_s_waitcnt(0x0F70);    // vmcnt(0): only copies are outstanding from here on
 #pragma unroll
     for (int i = 0; i < C::NCS; ++i) copy_scales(i, 0, sbase);
+    if constexpr (C::X4) edge(0, 0, C::NCX, true);
     for (int s = 0; s < C::NST - 1 && s < nk; ++s)
 #pragma unroll
         for (int u = 0; u < C::PER; ++u) issue(s, base + s * C::STAGE, u);
@@ -574,26 +599,21 @@ mx_tile(const Args a) {
         constexpr std::integral_constant<int, 2> HI{};
         static_assert(C::NST == 2 && C::SPC == 2 && C::KP == 4, "ring places and scale words of a slice");
         int s = 0;
-        // copy u of slice s + d (Q, CUT: of slice s, below)
-        auto copy = [&](auto Q, auto CUT, int d, int u) __attribute__((always_inline)) {
-            constexpr bool CUTS = decltype(CUT)::value;
+        constexpr int XA = C::AHEAD > C::NCP ? C::AHEAD - C::NCP : 0;   // copies of x among those two ahead
+        static_assert(XA <= C::NCX, "copies ahead");
+        // copy u of slice s + d (Q: of slice s, below)
+        auto copy = [&](auto Q, int d, int u) __attribute__((always_inline)) {
             const int q = Q, place = d == 1 ? 1 - q : q;
-            // behind K: chunk 0 of its row, of the last slice where the slice does not exist
-            const int left = nkb - (s + d) * 8;
-            const int none = max(s + d - nk + 1, 0) * 128;
-            auto back = [&](int c) __attribute__((always_inline)) { return CUTS && c >= left ? c * 16 : 0; };
-            int r;
             if (u < C::NCP) {
                 copy_scales((place * C::NCP + u) * C::NCS / (2 * C::NCP), (s + d) / 2 + 1,
                             base + (d == 2 || q ? r2 : r1));
             } else if (u < C::NCP + C::NCX) {
                 const int i = u - C::NCP;
-                dma16(px[i] - none - back(chunk_x(i, r)), base + place * C::STAGE + (wv + i * C::NW) * 1024);
+                dma16(px[i], base + place * C::STAGE + (wv + i * C::NW) * 1024);
                 px[i] += C::XROW;
             } else {
                 const int i = u - C::NCP - C::NCX;
-                dma16_at(weight(i) - none, ow[i] - back(chunk_w(i, r)),
-                         base + place * C::STAGE + C::X_BYTES + (wv + i * C::NW) * 1024);
+                dma16_at(weight(i), ow[i], base + place * C::STAGE + C::X_BYTES + (wv + i * C::NW) * 1024);
                 if (u == C::PER - 1)
 #pragma unroll
                     for (int b = 0; b < C::NB; ++b) bw[b] += C::WROW;
@@ -603,8 +623,8 @@ mx_tile(const Args a) {
         // of slice s + 1 before the last. Its copies go out beside the first two and the step
         // behind the barrier before those: spread out, for a wave whose copy waits for the
         // address unit issues no matrix instructions either. A scale word holds
-        // two pairs; words are read when those before them are used up. CUT: the slices behind may
-        // not exist, or slice s end early, with codes of zero and scales of 1.0 behind K then.
+        // two pairs; words are read when those before them are used up. CUT: K may end inside the
+        // slice, with codes of zero and scales of 1.0 behind it then.
         auto slice = [&](auto Q, auto CUT) __attribute__((always_inline)) {
             const int q = Q, t = 1 - q;
             constexpr bool CUTS = decltype(CUT)::value;
@@ -617,16 +637,23 @@ mx_tile(const Args a) {
                     for (int u = 0; u < NR; ++u) sc[u] = past ? 0x007f007fu : sc[u];
                 }
             };
+            // (the sums are pinned to this side of the branches, or their instructions would sink
+            // behind them and spill)
+#pragma unroll
+            for (int u = 0; u < C::NB * C::FM * C::FN; ++u)
+                asm volatile("" : "+v"(acc[u / (C::FM * C::FN)][u / C::FN % C::FM][u % C::FN]));
+            edge(s + 1, XA, C::NCX, true);
+            edge(s + 2, 0, XA, false);
             constexpr int P0 = C::AHEAD, P1 = P0 + (C::PER - P0 + 1) / 2;
             step(mma(f0, sa, LO), NR + P1 - P0, [&](int u) __attribute__((always_inline)) {
                 if (u < NR) read(q, 1, f1, u);
-                else copy(Q, CUT, 1, u - NR + P0);
+                else copy(Q, 1, u - NR + P0);
             });
             cut(1, f1, sa);
             constexpr int P2 = C::PER - P1;
             step(mma(f1, sa, HI), 2 * NR + P2, [&](int u) __attribute__((always_inline)) {
                 if (u < NR) read(q, 2, f0, u);
-                else if (u < NR + P2) copy(Q, CUT, 1, u - NR + P1);
+                else if (u < NR + P2) copy(Q, 1, u - NR + P1);
                 else sb[u - NR - P2] = read_scale(r0, r1, 2 * q + 1, u - NR - P2);
             });
             cut(2, f0, sb);
@@ -637,7 +664,7 @@ mx_tile(const Args a) {
             step(mma(f1, sb, HI), 2 * NR + P0, [&](int u) __attribute__((always_inline)) {
                 if (u < NR) read(t, 0, f0, u);
                 else if (u < 2 * NR) sa[u - NR] = read_scale(q ? r1 : r0, q ? r2 : r1, 2 * t, u - NR);
-                else copy(Q, CUT, 2, u - 2 * NR);
+                else copy(Q, 2, u - 2 * NR);
             });
         };
 #pragma unroll
@@ -645,21 +672,23 @@ mx_tile(const Args a) {
             sa[u] = read_scale(r0, r1, 0, u);
             read(0, 0, f0, u);
         }
+        constexpr std::integral_constant<int, 0> Q0{};
+        constexpr std::integral_constant<int, 1> Q1{};
+        edge(1, 0, XA, false);
 #pragma unroll
-        for (int u = 0; u < C::AHEAD; ++u) copy(0, std::true_type{}, 1, u);
-        // Whole chunks of two slices, with whole slices or none behind: places and copies are
-        // known at compile time (a loop that finds them out slice by slice issues twice as many
-        // instructions beside the matrix instructions, more than those hide).
-        const int behind = nkb % 8 ? 2 : 1;
-        for (; (s / 2 + behind) * 16 <= nkb; turn()) {
-            slice(std::integral_constant<int, 0>{}, std::false_type{});
+        for (int u = 0; u < C::AHEAD; ++u) copy(Q0, 1, u);
+        // Whole slices in pairs, then what is left: ring places are known at compile time (a loop
+        // that finds them out slice by slice issues twice as many instructions beside the matrix
+        // instructions, more than those hide).
+        for (; (s + 2) * 8 <= nkb; turn()) {
+            slice(Q0, std::false_type{});
             ++s;
-            slice(std::integral_constant<int, 1>{}, std::false_type{});
+            slice(Q1, std::false_type{});
             ++s;
         }
-        for (; s < nk; ++s) {
-            slice(s & 1, std::true_type{});
-            if (s & 1) turn();
+        if (s < nk) {
+            slice(Q0, std::true_type{});
+            if (++s < nk) slice(Q1, std::true_type{});
         }
         wait_vmcnt<0>();   // no copy may land behind the workgroup's end
     } else {
