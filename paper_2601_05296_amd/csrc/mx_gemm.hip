@@ -291,8 +291,8 @@ mx_stream(const Args a) {
 
 // ---- tile core --------------------------------------------------------------------------
 // Measured: 4-bit rows 4096 -> 14336 gated, eight experts, 3554 slots (444 rows each in tiles
-// of 256) 304 us, 2.75 PFLOP/s; 16384 slots 2.97; one 8192 x 8192 x 8192 product 3.6, where a
-// loop of the scaled instruction alone reaches 4.5. bfloat16 rows 2048 -> 1408 gated, 64 experts,
+// of 256) 289 us, 2.89 PFLOP/s; 16384 slots 1137, 3.38, where a loop of the scaled instruction
+// alone reaches 4.5. bfloat16 rows 2048 -> 1408 gated, 64 experts,
 // 98304 slots 975 to 1030 us, 1.1 to 1.16 PFLOP/s; 8192 x 8192 x 8192 1.28. About 12 (8) us of
 // a tile's time, its first copies and its results, run beside no matrix instruction: one
 // workgroup a CU.
@@ -813,23 +813,23 @@ hipError_t pick(const MxArgs& m, const Args& a, hipStream_t st) {
     // one (K = 4096, bfloat16 rows, one weight, tiles of 256, 128, 64 and 32 rows: 79, 49, 38, 16).
     // K -> N, rows of each of E experts; 256, 128, 64, 32 rows a tile:
     //                                        bfloat16 rows, one weight    4-bit rows, gated
-    //   4096 -> 14336   8 x  32                   -  118  76.2  62.7          -   112   103  99.2
-    //                   8 x  64                 188  125  83.0  92.0        150   118   115   124
-    //                   8 x 128                 198  133   145    -         160   133   174     -
-    //                   8 x 512                 412  459   517    -         296   394     -     -
-    //   14336 -> 4096   8 x 128                 262  216   155    -         135   121   163     -
-    //                   8 x 256                 299  243   261    -         154   192     -     -
-    //   4096 -> 4096    2 x 128                79.0 49.3  38.8  17.5       28.7  22.2  16.3  15.8
-    //                   2 x 256                78.8 49.7  39.9  25.1       31.8  22.6  18.8  28.7
-    //                   2 x 1024               85.9 65.8  74.3  89.5       41.9  47.9  63.6  79.6
-    //   2880 -> 2880    4 x 512                59.6 40.9  45.6  52.8       36.0  43.0  48.7  62.6
+    //   4096 -> 14336   8 x  32                   -  118  76.2  62.7        139   115   105  99.3
+    //                   8 x  64                 188  125  83.0  92.0        145   122   116   124
+    //                   8 x 128                 198  133   145    -         154   136   175   199
+    //                   8 x 512                 412  459   517    -         290   397   621   678
+    //   14336 -> 4096   8 x 128                 262  216   155    -         132   122   163   213
+    //                   8 x 256                 299  243   261    -         149   196   289   381
+    //   4096 -> 4096    2 x 128                79.0 49.3  38.8  17.5       27.0  22.2  18.2  15.3
+    //                   2 x 256                78.8 49.7  39.9  25.1       29.0  22.7  20.4  28.0
+    //                   2 x 1024               85.9 65.8  74.3  89.5       40.7  51.2  75.3  82.1
+    //   2880 -> 2880    4 x 512                59.6 40.9  45.6  52.8       31.6  42.1  48.7  61.4
     auto fills = [&](int bm, int bn) {
         return (double)active * std::ceil(rows / bm) * ((m.N + bn - 1) / bn) * 3.0 >= 2.0 * 256.0;
     };
     if (rows > 128 && fills(256, BN)) return tile<TCfg<256, BN, 2, 4, NB, X4, NST>>(m, a, st);
     if (rows > 64 && fills(128, BN)) return tile<TCfg<128, BN, 2, 4, NB, X4, NST>>(m, a, st);
     // With 4-bit rows half as many columns, twice the workgroups, where 64 rows: 4096 -> 14336,
-    // 8 x 48 rows 56.1, 58.8; 2048 -> 1408 gated, 64 x 48 rows 46.0, 49.3; bfloat16 rows, which
+    // 8 x 48 rows 56.9, 64.6; 2048 -> 1408 gated, 64 x 48 rows 47.2, 53.7; bfloat16 rows, which
     // four waves side by side convert once each: 98.3, 80.4; 70.4, 66.2.
     constexpr int BN64 = X4 ? BN / 2 : BN;
     if (rows > 32 && fills(64, BN64)) {
