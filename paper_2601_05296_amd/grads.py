@@ -7,10 +7,19 @@ import torch
 from . import binding as B
 from .layer import _on
 
+# what layer.backward gives beside the gradients of parameters
+NOT_PARAMETERS = ("dx", "dX_slot", "d_gates")
+
 
 def _list(grads):
-    """The tensors of a list, tuple or dict (as layer.backward returns), without None."""
-    return [g for g in (grads.values() if isinstance(grads, dict) else grads) if g is not None]
+    """The tensors of a list or tuple, without None; of a dict, as layer.backward returns, or of
+    dicts in the list, as block.backward's, the gradients of parameters."""
+    if isinstance(grads, dict):
+        return [g for n, g in grads.items() if g is not None and n not in NOT_PARAMETERS]
+    grads = [g for g in grads if g is not None]
+    if dict in map(type, grads):
+        return [t for g in grads for t in (_list(g) if isinstance(g, dict) else (g,))]
+    return grads
 
 
 def _norm(tl):
@@ -30,17 +39,18 @@ def _device(tl):
 
 def norm(grads, stream=None):
     """(norm, sumsq): the 2-norm over all elements of all tensors, float32, and its square,
-    float64, both on the GPU. Where a model's gradients are spread over several devices the
-    devices' sumsq add up."""
+    float64, both on the GPU. ``grads``: tensors, or the dict (dicts) of layer.backward
+    (block.backward), whose dx and d_gates, no parameters' gradients, stay out. Where a
+    model's gradients are spread over several devices the devices' sumsq add up."""
     with _on(stream):
         return _norm(B.TensorList(_list(grads)))
 
 
 def clip(grads, max_norm: float, out=None, sumsq=None, stream=None):
-    """Scale the gradients by min(1, max_norm / (norm + 1e-6)), in place or into ``out``
-    (tensors of the same sizes and types, in the same order). ``sumsq``: the square of the
-    norm to go by (a float64 GPU tensor: the sum over several devices'), None: these
-    tensors' own. Returns the norm, on the GPU; nothing waits for the host."""
+    """Scale the gradients (as in ``norm``) by min(1, max_norm / (norm + 1e-6)), in place or
+    into ``out`` (tensors of the same sizes and types, in the same order). ``sumsq``: the
+    square of the norm to go by (a float64 GPU tensor: the sum over several devices'),
+    None: these tensors' own. Returns the norm, on the GPU; nothing waits for the host."""
     with _on(stream):
         tl = B.TensorList(_list(grads))
         outs = None if out is None else B.TensorList(_list(out))

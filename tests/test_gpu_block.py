@@ -162,3 +162,39 @@ def test_stack_on_another_stream_and_in_a_graph():
         graph.replay()
         torch.cuda.synchronize()
         assert all(torch.equal(a, b) for a, b in zip(out, want)), i
+
+
+def test_two_streams_at_once():
+    """The same calls side by side on two streams, with workspaces and results of their own."""
+    g = torch.Generator(device="cuda").manual_seed(8)
+
+    def rnd(*s):
+        return torch.randn(*s, generator=g, device="cuda").to(torch.bfloat16)
+
+    T, d, E, f = 3000, 1024, 8, 768
+    w = [mx.quantize(rnd(E, f, d)) for _ in range(2)]
+    off = torch.arange(E + 1, device="cuda", dtype=torch.int32) * (T // E)
+    gate, wo, wr = rnd(d), rnd(d), rnd(d)
+    ins = [[rnd(T, d) for _ in range(4)] for _ in range(2)]
+
+    def calls(v):
+        o = block.norm_forward(v[0], v[1], gate, wo, wr)
+        b = block.norm_backward(v[2], v[3], v[1], o.r, o.rstd_post, o.rstd_pre, gate, wo, wr)
+        h = mx.product(o.n, w[0], off, None, w[1], "swiglu")
+        q = mx.product(mx.quantize(o.n), w[0], off)
+        out = [torch.empty_like(t) for t in (b["dw_pre"], h)]
+        n = grads.clip([b["dw_pre"], h], 0.5, out=out)
+        return [o.r, o.n, b["dres"], b["dy"], b["dgate"], b["dw_post"], b["dw_pre"], h, q, n, *out]
+
+    want = [calls(v) for v in ins]
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    got = [[], []]
+    for _ in range(4):
+        for i, st in enumerate(streams):
+            with torch.cuda.stream(st):
+                got[i].append(calls(ins[i]))
+    torch.cuda.synchronize()
+    for i in range(2):
+        for run in got[i]:
+            assert all(torch.equal(a, b) for a, b in zip(run, want[i])), i

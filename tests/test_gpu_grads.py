@@ -111,6 +111,11 @@ def test_lists_dicts_none_and_nothing():
     t = _rand(100, F32)
     total, _ = grads.norm(dict(a=t, b=None))
     assert torch.equal(total, grads.norm([t])[0])
+    u = _rand(33, BF)
+    layers = [dict(dw1=t, dx=_rand(50, BF), d_gates=_rand(7, F32), dw3=None), dict(dX_slot=_rand(9, BF), dw1=u)]
+    assert torch.equal(grads.norm(layers[0])[0], grads.norm([t])[0])
+    assert torch.equal(grads.norm(layers)[0], grads.norm([t, u])[0])
+    assert torch.equal(grads.norm([t, layers[1]])[0], grads.norm([t, u])[0])
     total, sumsq = grads.norm([])
     assert float(total) == 0.0 and float(sumsq) == 0.0
     assert float(grads.clip([None], 1.0)) == 0.0
