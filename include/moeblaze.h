@@ -61,8 +61,9 @@ extern "C" {
  * non-gated expert of Section 2.2, E(x) = w2 act(x w1) (ReLU and SiLU are the
  * activations of the experiments, Section 6): w3, B and dw3 are then unused
  * and may be NULL, A = x w1 is the only saved activation and act is
- * recomputed from it in the backward. ReLU'(0) is taken as 0. At most one of
- * the two may be set (else MOE_ERR_INVALID_ARG). */
+ * recomputed from it in the backward. ReLU'(0) is taken as 0, and the ReLU of a
+ * NaN as 0 with gradient 0 (moe_mx_gemm keeps it NaN). At most one of the two
+ * may be set (else MOE_ERR_INVALID_ARG). */
 #define MOE_ACT_SILU    8u
 #define MOE_ACT_RELU    16u
 /* The FFN calls and their workspace queries: buffer no h = SiLU(A) * B.
@@ -439,8 +440,10 @@ int moe_mx_dequantize(const void* codes, const void* scales, int64_t R, int K, u
  * Out: out [S,N] bfloat16. Rows at or behind offsets[E] are left as they were.
  * Limits: K and N multiples of 64, N K < 2^33, E <= 256, S < 2^31, T < 2^31; rows
  * NULL: T == S.
- * The scales 0 to 254 stand for 2^(s - 127), 255 for NaN. Scales are read in
- * whole aligned 4-byte words: where T K/32 is not a multiple of 4, up to two
+ * The scales 0 to 254 stand for 2^(s - 127), 255 for NaN, which every activation
+ * keeps: a NaN in a row of x reaches that row's slots, one in a row of w that column
+ * of its expert. Scales are read in whole
+ * aligned 4-byte words: where T K/32 is not a multiple of 4, up to two
  * bytes behind the last of x_scales are read (and not used). No workspace.
  */
 int moe_mx_gemm(const void* x, const void* x_scales, const void* w, const void* w_scales,

@@ -40,11 +40,12 @@ __device__ __forceinline__ f32x16 mfma_mx32(const uint4& p, uint32_t sp, const u
     return __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(fp4_operand(p), fp4_operand(q), c, 4, 4, BYTE, (int)sp, BYTE, (int)sq);
 }
 
-// the activation of one sum (a pair of sums for SwiGLU), in float32
+// the activation of one sum (a pair of sums for SwiGLU), in float32. A NaN sum stays NaN, also
+// under ReLU, where fmaxf would give zero: a weight block that held an infinity has the NaN scale.
 template <int NB>
 __device__ __forceinline__ float activate(float a, float b, int act) {
     if constexpr (NB == 2) return a * sigmoidf_(a) * b;
-    return act == 1 ? a * sigmoidf_(a) : act == 2 ? fmaxf(a, 0.f) : a;
+    return act == 1 ? a * sigmoidf_(a) : act == 2 ? (a <= 0.f ? 0.f : a) : a;
 }
 
 struct Args {
