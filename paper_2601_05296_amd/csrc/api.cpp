@@ -508,7 +508,8 @@ int moe_norm_bwd(const void* dr, const void* dn, const void* y, const void* r, c
     const bool post = flags & MOE_NORM_POST, pre = flags & MOE_NORM_PRE;
     FLAG_PTR(w_post, post, "MOE_NORM_POST"); FLAG_PTR(dw_post, post, "MOE_NORM_POST");
     FLAG_PTR(w_pre, pre, "MOE_NORM_PRE"); FLAG_PTR(dw_pre, pre, "MOE_NORM_PRE");
-    FLAG_PTR(dgate, kind, "a gate flag");
+    // without rows a token's or a full gate has no element, and its address may be NULL
+    if (T > 0 || kind < 2) FLAG_PTR(dgate, kind, "a gate flag");
     if (T > 0) {
         if (!dy && (e = check_no_block(fn, res_scale, flags))) return e;
         if (!dr && !pre) return fail(MOE_ERR_INVALID_ARG, "%s: neither dr nor MOE_NORM_PRE: no gradient comes in", fn);

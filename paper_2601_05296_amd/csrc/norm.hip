@@ -507,6 +507,7 @@ hipError_t norm_bwd(const NormArgs& a, hipStream_t st) {
     const BwdArgs k{a.dr, a.dn, a.y, a.r, a.gate, a.w_post, a.w_pre, a.rstd_post, a.rstd_pre,
                     a.dres, a.dy, a.dgate, a.part, a.res_scale, a.T, a.d, a.gate_kind};
     const bool sums = a.w_pre || a.w_post || a.gate_kind == GATE_CHANNEL;
+    if (a.T == 0 && !sums) return hipSuccess;
     if (a.T > 0) {
         if (a.f32) launch_bwd<true>(k, st);
         else launch_bwd<false>(k, st);

@@ -1,0 +1,20 @@
+"""CPU checks at the edges of what the operators around the layer take."""
+from paper_2601_05296_amd import binding as B
+
+FAKE = 1 << 20   # aligned, never dereferenced
+
+
+def test_norm_bwd_of_no_rows_needs_no_gate_gradient():
+    """The gradient of a token's or a full gate has no element then; an empty tensor's address
+    is NULL. A channel's is summed over the rows, and written."""
+    lib = B.load_library()
+
+    def bwd(flags, dgate):
+        return lib.moe_norm_bwd(None, None, None, None, None, None, None, None, None, 1.0, 0, 64, flags, None,
+                                None, dgate, None, None, None, 0, None)
+
+    tok, chan = B.MOE_GATE_TOKEN, B.MOE_GATE_CHANNEL
+    for fl in (tok, tok | chan, tok | B.MOE_F32):
+        assert bwd(fl, None) == B.MOE_OK and bwd(fl, FAKE) == B.MOE_OK
+    assert bwd(chan, None) == B.MOE_ERR_INVALID_ARG and b"dgate is NULL" in lib.moe_last_error()
+    assert bwd(0, FAKE) == B.MOE_ERR_INVALID_ARG and b"dgate without" in lib.moe_last_error()

@@ -1,12 +1,15 @@
 """Calls at the edges of what the operators around the layer take."""
+import math
+
 import numpy as np
 import pytest
 import torch
 
-from paper_2601_05296_amd import mx
+from paper_2601_05296_amd import block, mx
 from tests.test_gpu_mx import WIDE, _case
 
 pytestmark = pytest.mark.gpu
+BF, F32 = torch.bfloat16, torch.float32
 
 
 @pytest.mark.parametrize("act", ["none", "relu", "silu", "swiglu"])
@@ -28,3 +31,25 @@ def test_product_keeps_nan_under_every_activation(act, x4, counts, N):
     nan[0] = True
     assert np.array_equal(np.isnan(out), nan)
     assert (np.abs(out - ref)[~nan] <= tol[~nan]).all()
+
+
+@pytest.mark.parametrize("gate", [None, "channel", "token", "full"])
+@pytest.mark.parametrize("post,pre", [(True, True), (False, True), (True, False)])
+@pytest.mark.parametrize("dt", [BF, F32])
+def test_norms_of_no_rows(gate, post, pre, dt):
+    """An empty batch: empty tensors, and zeros for what is summed over the rows."""
+    d = 64
+    none, w = torch.empty(0, d, dtype=dt, device="cuda"), torch.ones(d, dtype=dt, device="cuda")
+    g = {None: None, "channel": w, "token": none[:, :1].contiguous(), "full": none}[gate]
+    o = block.norm_forward(none, none, g, w if post else None, w if pre else None)
+    assert o.r.shape == (0, d)
+    junk = [torch.full((d,), math.nan, device="cuda") for _ in range(8)]
+    torch.cuda.synchronize()
+    del junk
+    b = block.norm_backward(none, none if pre else None, none, o.r, o.rstd_post, o.rstd_pre, g,
+                            w if post else None, w if pre else None)
+    assert b["dres"].shape == b["dy"].shape == (0, d)
+    for k, on in (("dw_post", post), ("dw_pre", pre)):
+        assert (b[k] is not None) == on and (not on or (b[k].shape == (d,) and not b[k].any()))
+    if gate is not None:
+        assert b["dgate"].shape == g.shape and not b["dgate"].any()
