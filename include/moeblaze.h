@@ -388,10 +388,11 @@ int moe_norm_bwd(const void* dr, const void* dn, const void* y, const void* r, c
  * moe_grad_clip -- out[i] = c * grads[i] with
  *   c = min(1, max_norm / (sqrt(*sumsq) + 1e-6))   (sumsq on the device),
  * so that the list's norm is at most max_norm. A NaN in sumsq makes c and every
- * output NaN; an infinite one makes c zero. outs NULL: in place, and with c == 1
- * nothing is read or written. Else each out tensor is its gradient itself or
- * overlaps no tensor of the call (MOE_ERR_INVALID_ARG, as for two gradients that
- * overlap while one is written). max_norm >= 0 (infinity: c = 1).
+ * output NaN; an infinite one makes c zero (and infinite elements NaN), but not
+ * against an infinite max_norm, where c is 1 unless sumsq is NaN. outs NULL: in
+ * place, and with c == 1 nothing is read or written. Else each out tensor is its
+ * gradient itself or overlaps no tensor of the call (MOE_ERR_INVALID_ARG, as for
+ * two gradients that overlap while one is written). max_norm >= 0.
  */
 size_t moe_grad_norm_workspace_size(int n);
 int moe_grad_norm(const void* const* grads, const int64_t* sizes, const unsigned* types, int n,

@@ -189,8 +189,9 @@ __device__ __forceinline__ void chunk_scale(const Entry& e, int64_t c, float k) 
 
 __global__ void __launch_bounds__(GT)
 grad_scale(const Table t, const double* __restrict__ sumsq, double max_norm) {
-    const double r = max_norm / (sqrt(*sumsq) + 1e-6);
-    const float k = r >= 1.0 ? 1.0f : (float)r;   // NaN stays
+    // a norm up to the limit, an infinite one up to an infinite limit: unchanged; NaN stays
+    const double norm = sqrt(*sumsq) + 1e-6;
+    const float k = norm <= max_norm ? 1.0f : (float)(max_norm / norm);
     for (int64_t c = blockIdx.x; c < t.first[t.n]; c += gridDim.x) {
         const int i = find(t, c);
         const Entry e = t.t[i];

@@ -50,7 +50,8 @@ def clip(grads, max_norm: float, out=None, sumsq=None, stream=None):
     """Scale the gradients (as in ``norm``) by min(1, max_norm / (norm + 1e-6)), in place or
     into ``out`` (tensors of the same sizes and types, in the same order). ``sumsq``: the
     square of the norm to go by (a float64 GPU tensor: the sum over several devices'),
-    None: these tensors' own. Returns the norm, on the GPU; nothing waits for the host."""
+    None: these tensors' own. ``max_norm`` infinite: the norm alone is of use, nothing is
+    scaled. Returns the norm, on the GPU; nothing waits for the host."""
     with _on(stream):
         tl = B.TensorList(_list(grads))
         outs = None if out is None else B.TensorList(_list(out))

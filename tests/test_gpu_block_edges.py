@@ -5,7 +5,7 @@ import numpy as np
 import pytest
 import torch
 
-from paper_2601_05296_amd import block, mx
+from paper_2601_05296_amd import block, grads, mx
 from tests.test_gpu_mx import WIDE, _case
 
 pytestmark = pytest.mark.gpu
@@ -53,3 +53,20 @@ def test_norms_of_no_rows(gate, post, pre, dt):
         assert (b[k] is not None) == on and (not on or (b[k].shape == (d,) and not b[k].any()))
     if gate is not None:
         assert b["dgate"].shape == g.shape and not b["dgate"].any()
+
+
+def test_clip_by_an_infinite_limit():
+    """max_norm infinite leaves every gradient as it is, infinite ones among them; a NaN in the
+    norm makes all NaN, also then."""
+    a = torch.randn(5000, device="cuda")
+    b = torch.randn(301, device="cuda").to(BF)
+    a[4321], b[7] = math.inf, -math.inf
+    for dst in (None, [torch.empty_like(a), torch.empty_like(b)]):
+        g = [a.clone(), b.clone()]
+        total = grads.clip(g, math.inf, out=dst)
+        assert float(total) == math.inf
+        assert torch.equal((dst or g)[0], a) and torch.equal((dst or g)[1], b)
+    g = [a.clone(), b.clone()]
+    g[0][1] = math.nan
+    assert math.isnan(float(grads.clip(g, math.inf)))
+    assert torch.isnan(g[0]).all() and torch.isnan(g[1]).all()
