@@ -8,7 +8,7 @@ from . import binding as B
 from .layer import _on
 
 # what layer.backward gives beside the gradients of parameters
-NOT_PARAMETERS = ("dx", "dX_slot", "d_gates")
+NOT_PARAMETERS = ("dx", "dX_slot", "dx_ffn", "d_gates")
 
 
 def _list(grads):
@@ -40,8 +40,8 @@ def _device(tl):
 def norm(grads, stream=None):
     """(norm, sumsq): the 2-norm over all elements of all tensors, float32, and its square,
     float64, both on the GPU. ``grads``: tensors, or the dict (dicts) of layer.backward
-    (block.backward), whose dx and d_gates, no parameters' gradients, stay out. Where a
-    model's gradients are spread over several devices the devices' sumsq add up."""
+    (block.backward), whose NOT_PARAMETERS stay out. Where a model's gradients are spread over
+    several devices the devices' sumsq add up."""
     with _on(stream):
         return _norm(B.TensorList(_list(grads)))
 

@@ -1,5 +1,8 @@
 """CPU checks at the edges of what the operators around the layer take."""
+import torch
+
 from paper_2601_05296_amd import binding as B
+from paper_2601_05296_amd import grads
 
 FAKE = 1 << 20   # aligned, never dereferenced
 
@@ -18,3 +21,11 @@ def test_norm_bwd_of_no_rows_needs_no_gate_gradient():
         assert bwd(fl, None) == B.MOE_OK and bwd(fl, FAKE) == B.MOE_OK
     assert bwd(chan, None) == B.MOE_ERR_INVALID_ARG and b"dgate is NULL" in lib.moe_last_error()
     assert bwd(0, FAKE) == B.MOE_ERR_INVALID_ARG and b"dgate without" in lib.moe_last_error()
+
+
+def test_gradients_of_parameters_alone():
+    """What layer.backward(keep=True) adds beside the parameters' gradients stays out of a norm."""
+    par = {n: torch.ones(3) for n in ("dw1", "dw3", "dw2", "dw_gate")}
+    rest = {n: torch.ones(5) for n in ("dx", "dX_slot", "dx_ffn", "d_gates")}
+    assert [t.numel() for t in grads._list({**rest, **par})] == [3] * 4
+    assert [t.numel() for t in grads._list([{**par, **rest}, rest, par["dw1"]])] == [3] * 5

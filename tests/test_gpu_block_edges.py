@@ -5,7 +5,7 @@ import numpy as np
 import pytest
 import torch
 
-from paper_2601_05296_amd import block, grads, mx
+from paper_2601_05296_amd import block, grads, layer, mx
 from tests.test_gpu_mx import WIDE, _case
 
 pytestmark = pytest.mark.gpu
@@ -70,3 +70,25 @@ def test_clip_by_an_infinite_limit():
     g[0][1] = math.nan
     assert math.isnan(float(grads.clip(g, math.inf)))
     assert torch.isnan(g[0]).all() and torch.isnan(g[1]).all()
+
+
+def _layer(T, dt=BF, act="swiglu"):
+    g = torch.Generator(device="cuda").manual_seed(T)
+
+    def rnd(*s):
+        return (0.2 * torch.randn(*s, generator=g, device="cuda")).to(dt)
+
+    return rnd(T, 64), rnd(4, 64), rnd(4, 64, 128), rnd(4, 64, 128) if act == "swiglu" else None, rnd(4, 128, 64)
+
+
+def test_norm_of_all_that_a_backward_returns():
+    """With keep=True the backward returns dX_slot and its sum over slots too: no parameters'."""
+    x, wg, w1, w3, w2 = _layer(40)
+    y, saved = layer.forward(x, wg, None, w1, w3, w2, 2, False, separate=True)
+    g = layer.backward(saved, y, x, wg, w1, w3, w2, keep=True)
+    par = [g[n] for n in ("dw1", "dw3", "dw2", "dw_gate")]
+    assert torch.equal(grads.norm(g)[1], grads.norm(par)[1])
+    before = {n: t.clone() for n, t in g.items()}
+    grads.clip(g, 1e-3)
+    for n, t in g.items():
+        assert torch.equal(t, before[n]) == (n in ("dx", "dX_slot", "dx_ffn", "d_gates")), n
