@@ -117,9 +117,9 @@ def aligned_chunk(chunk: int, T: int) -> int:
     """A chunk of T tokens as the chunked calls take it: all of T, or a
     multiple of 4 tokens (at least 4), so that every chunk's rows of the
     [T, k] routing arrays (4-byte elements) start 16-byte aligned, as the C
-    ABI requires of its pointers."""
+    ABI requires of its pointers. Without tokens: 1, and there is no chunk."""
     if chunk >= T:
-        return T
+        return max(T, 1)
     return max(4, chunk - chunk % 4)
 
 
@@ -286,7 +286,8 @@ def backward(saved: Saved, dy, x, w_gate, w1, w3, w2, stream=None, keep=False,
     """Returns dict(dx, dw_gate, dw1, dw3, dw2, d_gates[, dX_slot]). Overwrites
     saved.A / saved.B with dA / dB. dw3 is None for a non-gated expert.
     ``keep`` (returns dX_slot and the FFN part of dx) implies ``separate``.
-    Everything runs on ``stream`` (torch's current stream if None)."""
+    Without tokens the weights' gradients are zeros. Everything runs on ``stream``
+    (torch's current stream if None)."""
     with _on(stream):
         return _backward(saved, dy, x, w_gate, w1, w3, w2, keep, separate)
 
@@ -321,6 +322,17 @@ def _backward_recompute(s, dy, x, w_gate, w1, w3, w2):
     return dict(dw1=dw1, dw3=dw3, dw2=dw2, d_gates=d_gates), dx
 
 
+def _backward_empty(s, dy, keep):
+    z = dict(dtype=torch.float32, device=dy.device)
+    d, f, E = s.d, s.f, s.E
+    out = dict(dw1=torch.zeros((E, d, f), **z), dw3=torch.zeros((E, d, f), **z) if s.act == "swiglu" else None,
+               dw2=torch.zeros((E, f, d), **z), d_gates=torch.empty((0, s.k), **z))
+    if keep:
+        out.update(dX_slot=torch.empty_like(dy), dx_ffn=torch.empty_like(dy))
+    out.update(dx=torch.empty_like(dy), dw_gate=torch.zeros((E, d), **z))
+    return out
+
+
 def _backward(saved, dy, x, w_gate, w1, w3, w2, keep, separate):
     stream = None   # torch's current stream, set by backward()
     s = saved
@@ -328,9 +340,11 @@ def _backward(saved, dy, x, w_gate, w1, w3, w2, keep, separate):
     dev = dy.device
     f32 = dict(dtype=torch.float32, device=dev)
     gated = s.act == "swiglu"
+    if s.chunk and (keep or separate):
+        raise ValueError("the full-recompute policy runs the combined calls only")
+    if T == 0:   # the library's calls write nothing then
+        return _backward_empty(s, dy, keep)
     if s.chunk:   # full recompute
-        if keep or separate:
-            raise ValueError("the full-recompute policy runs the combined calls only")
         out, dx = _backward_recompute(s, dy, x, w_gate, w1, w3, w2)
         return _router_backward(s, x, w_gate, out, dx)
     dw1 = torch.empty((E, d, f), **f32)

@@ -2,7 +2,7 @@
 import torch
 
 from paper_2601_05296_amd import binding as B
-from paper_2601_05296_amd import grads
+from paper_2601_05296_amd import grads, layer
 
 FAKE = 1 << 20   # aligned, never dereferenced
 
@@ -29,3 +29,8 @@ def test_gradients_of_parameters_alone():
     rest = {n: torch.ones(5) for n in ("dx", "dX_slot", "dx_ffn", "d_gates")}
     assert [t.numel() for t in grads._list({**rest, **par})] == [3] * 4
     assert [t.numel() for t in grads._list([{**par, **rest}, rest, par["dw1"]])] == [3] * 5
+
+
+def test_no_tokens_make_no_chunk():
+    for want in (1, 4, 100):
+        assert list(layer._chunks(0, layer.aligned_chunk(want, 0))) == []

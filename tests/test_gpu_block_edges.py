@@ -92,3 +92,45 @@ def test_norm_of_all_that_a_backward_returns():
     grads.clip(g, 1e-3)
     for n, t in g.items():
         assert torch.equal(t, before[n]) == (n in ("dx", "dX_slot", "dx_ffn", "d_gates")), n
+
+
+@pytest.mark.parametrize("dt", [BF, F32])
+@pytest.mark.parametrize("act", ["swiglu", "relu"])
+@pytest.mark.parametrize("recompute", [False, True])
+def test_stack_of_no_rows(dt, act, recompute):
+    """A stack on an empty batch: an empty stream, and a zero gradient for every parameter."""
+    bl = []
+    for i in range(2):
+        _, wg, w1, w3, w2 = _layer(i + 1, dt, act)
+        one = torch.ones(64, dtype=dt, device="cuda")
+        bl.append(block.Block(one, wg, w1, w3, w2, k=2, act=act, gate=one, w_post=one))
+    x = torch.empty(0, 64, dtype=dt, device="cuda")
+    y, saved = block.forward(bl, x, recompute=recompute)
+    junk = [torch.full(s, math.nan, device="cuda") for s in ((4, 64, 128), (4, 64), (64,)) for _ in range(12)]
+    torch.cuda.synchronize()
+    del junk
+    dx, g = block.backward(bl, saved, y)
+    assert y.shape == dx.shape == (0, 64)
+    for gb in g:
+        assert {"dw1", "dw2", "dw_gate", "dgate", "dw_pre", "dw_post"} <= set(gb)
+        for n, t in gb.items():
+            assert t is None and n == "dw3" and act == "relu" or not t.any(), n
+    assert float(grads.clip(g, 1.0)) == 0.0
+    if dt == BF:
+        for b in bl:
+            b.experts = mx.quantize_experts(b.w1, b.w3, b.w2)
+        for rows in ("bf16", "mx"):
+            assert block.infer(bl, x, rows=rows).shape == (0, 64)
+
+
+def test_layer_of_no_rows_returns_what_others_do():
+    """The same keys, shapes and types as with tokens, whatever was asked to be kept."""
+    for T in (3, 0):
+        x, wg, w1, w3, w2 = _layer(3)
+        x = x[:T].contiguous()
+        y, saved = layer.forward(x, wg, None, w1, w3, w2, 2, False, separate=True)
+        g = layer.backward(saved, y, x, wg, w1, w3, w2, keep=True)
+        got = {n: (tuple(t.shape), t.dtype) for n, t in g.items()}
+        if T:
+            want = {n: ((0,) + s[1:] if s[0] in (3, 6) else s, dt) for n, (s, dt) in got.items()}
+    assert list(got) == list(want) and got == want
