@@ -413,11 +413,11 @@ int moe_grad_clip(const void* const* grads, void* const* outs, const int64_t* si
  * In:  src [batch, R, K], or with MOE_TRANSPOSED [batch, K, R] (the layout of
  *      w1, w3, w2: K is the axis that a product sums over); MOE_F32 / MOE_BF16.
  * Out: codes [batch, R, K/2] bytes, scales [batch, R, K/32] bytes.
- * K a multiple of 32; fewer than 2^36 values; MOE_TRANSPOSED: R even and below
- * 2^29, batch <= 65535, K <= 2^24.
+ * K a multiple of 32; at most 2^36 - 4096 values; MOE_TRANSPOSED: R even, at most
+ * 2^29 - 128, batch <= 65535, K <= 2^24.
  *
  * moe_mx_dequantize -- out [R, K] = the values of codes [R, K/2] under scales
- * [R, K/32] (any bytes), bfloat16 or MOE_F32.
+ * [R, K/32] (any bytes), bfloat16 or MOE_F32. Fewer than 2^36 values.
  */
 int moe_mx_quantize(const void* src, int64_t batch, int64_t R, int K, unsigned flags,
                     void* codes, void* scales, hipStream_t stream);

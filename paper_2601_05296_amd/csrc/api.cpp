@@ -644,12 +644,14 @@ int moe_mx_quantize(const void* src, int64_t batch, int64_t R, int K, unsigned f
     if (batch < 0 || R < 0) return fail(MOE_ERR_INVALID_ARG, "%s: batch = %lld, R = %lld", fn, (long long)batch, (long long)R);
     if (K < 1) return fail(MOE_ERR_INVALID_ARG, "%s: K = %d < 1", fn, K);
     if (K % 32) return fail(MOE_ERR_UNSUPPORTED, "%s: K = %d is not a multiple of 32", fn, K);
-    if ((double)batch * (double)R * K >= 68719476736.0)
-        return fail(MOE_ERR_UNSUPPORTED, "%s: 2^36 values or more", fn);
+    // a launch has fewer than 2^32 threads: 16 values each, 256 a workgroup
+    if ((double)batch * (double)R * K > 68719476736.0 - 4096.0)
+        return fail(MOE_ERR_UNSUPPORTED, "%s: more than 2^36 - 4096 values", fn);
     if (flags & MOE_TRANSPOSED) {
         if (R % 2) return fail(MOE_ERR_UNSUPPORTED, "%s: R = %lld is odd (MOE_TRANSPOSED)", fn, (long long)R);
         if (batch > 65535) return fail(MOE_ERR_UNSUPPORTED, "%s: batch = %lld > 65535 (MOE_TRANSPOSED)", fn, (long long)batch);
-        if (R >= (1 << 29)) return fail(MOE_ERR_UNSUPPORTED, "%s: R = %lld, 2^29 or more (MOE_TRANSPOSED)", fn, (long long)R);
+        // 1024 threads for 128 columns
+        if (R > (1 << 29) - 128) return fail(MOE_ERR_UNSUPPORTED, "%s: R = %lld > 2^29 - 128 (MOE_TRANSPOSED)", fn, (long long)R);
         if (K > (1 << 24)) return fail(MOE_ERR_UNSUPPORTED, "%s: K = %d > 2^24 (MOE_TRANSPOSED)", fn, K);
     }
     if (batch == 0 || R == 0) return MOE_OK;

@@ -34,3 +34,16 @@ def test_gradients_of_parameters_alone():
 def test_no_tokens_make_no_chunk():
     for want in (1, 4, 100):
         assert list(layer._chunks(0, layer.aligned_chunk(want, 0))) == []
+
+
+def test_quantize_refuses_what_no_launch_covers():
+    """Sizes whose grid would need 2^32 threads: refused before the launch, not failed by it."""
+    lib = B.load_library()
+
+    def quant(batch, rows, K, flags=0):
+        return lib.moe_mx_quantize(FAKE, batch, rows, K, flags, FAKE, FAKE, None)
+
+    assert quant(1, (1 << 31) - 1, 32) == B.MOE_ERR_UNSUPPORTED and b"2^36 - 4096" in lib.moe_last_error()
+    assert quant(1, (1 << 31) - 127, 32, B.MOE_F32) == B.MOE_ERR_UNSUPPORTED
+    for rows in ((1 << 29) - 126, (1 << 29) - 2):
+        assert quant(1, rows, 32, B.MOE_TRANSPOSED) == B.MOE_ERR_UNSUPPORTED and b"2^29 - 128" in lib.moe_last_error()

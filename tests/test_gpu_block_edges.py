@@ -134,3 +134,14 @@ def test_layer_of_no_rows_returns_what_others_do():
         if T:
             want = {n: ((0,) + s[1:] if s[0] in (3, 6) else s, dt) for n, (s, dt) in got.items()}
     assert list(got) == list(want) and got == want
+
+
+def test_quantize_the_largest_width():
+    """The widest transposed matrix that is taken, its last columns against the same alone."""
+    R = (1 << 29) - 128
+    x = torch.zeros(32, R, dtype=BF, device="cuda")
+    tail = torch.randn(32, 10, generator=torch.Generator().manual_seed(0)).to(BF).cuda()
+    x[:, -10:] = tail
+    q, w = mx.quantize(x, True), mx.quantize(tail, True)
+    assert torch.equal(q.codes[-10:], w.codes) and torch.equal(q.scales[-10:], w.scales)
+    assert not q.codes[:-10].any() and not q.scales[:-10].any()
