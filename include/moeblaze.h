@@ -440,12 +440,17 @@ int moe_mx_dequantize(const void* codes, const void* scales, int64_t R, int K, u
  *      [E,N,K/32] (w3 with MOE_GATED, else NULL); offsets [E+1], rows [S] int32.
  * Out: out [S,N] bfloat16. Rows at or behind offsets[E] are left as they were.
  * Limits: K and N multiples of 64, N K < 2^33, E <= 256, S < 2^31, T < 2^31; rows
- * NULL: T == S.
+ * NULL: T == S. (Beyond an S N of about 2^36 a grid may not be launchable:
+ * MOE_ERR_HIP.)
+ * Whatever offsets and rows hold, nothing outside the tensors is written, and read
+ * no more than two bytes: a row index outside x reads its last row, and offsets that
+ * decrease, are negative or pass S leave rows of out undefined.
  * The scales 0 to 254 stand for 2^(s - 127), 255 for NaN, which every activation
  * keeps: a NaN in a row of x reaches that row's slots, one in a row of w that column
- * of its expert. Scales are read in whole
- * aligned 4-byte words: where T K/32 is not a multiple of 4, up to two
- * bytes behind the last of x_scales are read (and not used). No workspace.
+ * of its expert. With bfloat16 rows a weight of 2^128 or more (scales 253 and 254,
+ * which moe_mx_quantize does not write) is infinite. Scales are read in whole
+ * aligned 4-byte words: where T K/32 is not a multiple of 4, up to two bytes behind
+ * the last of x_scales are read (and not used). No workspace.
  */
 int moe_mx_gemm(const void* x, const void* x_scales, const void* w, const void* w_scales,
                 const void* w3, const void* w3_scales, const int32_t* offsets,

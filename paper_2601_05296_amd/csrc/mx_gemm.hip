@@ -54,7 +54,7 @@ struct Args {
     const uint8_t *w[2], *ws[2];
     const int32_t *offsets, *rows;
     int64_t T;
-    int N, K, E, act;
+    int S, N, K, E, act;
     bf16_t* out;
 };
 
@@ -62,6 +62,17 @@ struct Args {
 __device__ __forceinline__ int64_t x_row(const Args& a, int slot) {
     const uint32_t r = a.rows ? (uint32_t)a.rows[slot] : (uint32_t)slot;
     return min((int64_t)r, a.T - 1);
+}
+
+// Whether a tile has anything to compute. Its rows end with the result's: offsets are a caller's
+// data, and whatever they hold, no slot outside [0, S) and no weight outside w is touched.
+__device__ __forceinline__ bool inside(const Args& a, SlotTile& t) {
+    const uint32_t slot = (uint32_t)t.off + (uint32_t)t.m0;
+    if ((t.off | t.m0) < 0 || slot >= (uint32_t)a.S || (uint32_t)t.n0 >= (uint32_t)a.N ||
+        (uint32_t)t.e >= (uint32_t)a.E)
+        return false;
+    t.mrows = min(t.mrows, a.S - (int)slot);
+    return t.mrows > 0;
 }
 
 // ---- stream core ------------------------------------------------------------------------
@@ -112,7 +123,8 @@ mx_stream(const Args a) {
     extern __shared__ __attribute__((aligned(16))) char lds[];
     SlotTile t;
     if (!find_slot_tile<C::THREADS>(reinterpret_cast<int*>(lds), a.offsets, a.E, C::BM,
-                                    (a.N + C::BN - 1) / C::BN, blockIdx.x, C::BN, t))
+                                    (a.N + C::BN - 1) / C::BN, blockIdx.x, C::BN, t) ||
+        !inside(a, t))
         return;
     const int lane = threadIdx.x & 63, wv = wave_id();
     const int r16 = lane & 15, g = lane >> 4, wn = wv % C::WN, wk = wv / C::WN;
@@ -375,7 +387,8 @@ mx_tile(const Args a) {
     extern __shared__ __attribute__((aligned(16))) char lds[];
     SlotTile t;
     if (!find_slot_tile<C::THREADS>(reinterpret_cast<int*>(lds), a.offsets, a.E, C::BM,
-                                    (a.N + C::BN - 1) / C::BN, blockIdx.x, C::BN, t, 4))
+                                    (a.N + C::BN - 1) / C::BN, blockIdx.x, C::BN, t, 4) ||
+        !inside(a, t))
         return;
     const int lane = threadIdx.x & 63, wv = wave_id();
     const int wm = wv / C::WN, wn = wv % C::WN;
@@ -867,8 +880,8 @@ hipError_t pick(const MxArgs& m, const Args& a, hipStream_t st) {
 }  // namespace
 
 hipError_t mx_gemm(const MxArgs& m, hipStream_t st) {
-    const Args a{m.x, m.xs, {m.w, m.w3}, {m.ws, m.ws3}, m.offsets, m.rows, m.T, m.N, m.K, m.E, m.act,
-                 static_cast<bf16_t*>(m.out)};
+    const Args a{m.x, m.xs, {m.w, m.w3}, {m.ws, m.ws3}, m.offsets, m.rows, m.T, (int)m.S, m.N, m.K, m.E,
+                 m.act, static_cast<bf16_t*>(m.out)};
     if (m.xs) return m.w3 ? pick<true, 2>(m, a, st) : pick<true, 1>(m, a, st);
     return m.w3 ? pick<false, 2>(m, a, st) : pick<false, 1>(m, a, st);
 }

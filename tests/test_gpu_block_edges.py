@@ -5,6 +5,7 @@ import numpy as np
 import pytest
 import torch
 
+from paper_2601_05296_amd import binding as B
 from paper_2601_05296_amd import block, grads, layer, mx
 from tests.test_gpu_mx import WIDE, _case
 
@@ -145,3 +146,47 @@ def test_quantize_the_largest_width():
     q, w = mx.quantize(x, True), mx.quantize(tail, True)
     assert torch.equal(q.codes[-10:], w.codes) and torch.equal(q.scales[-10:], w.scales)
     assert not q.codes[:-10].any() and not q.scales[:-10].any()
+
+
+# rows of each expert, N: each core (few rows, 16 and 32 rows, tiles)
+CORES = [([1, 0, 1], 64), ([9, 2], 64), ([25, 30], 128), ([90, 40, 70, 80], WIDE)]
+
+
+@pytest.mark.parametrize("x4", [False, True])
+@pytest.mark.parametrize("counts,N", CORES)
+def test_product_ends_with_its_slots(x4, counts, N):
+    """offsets that begin behind slot 0 (slots before are left as they were), and offsets that
+    go on behind the S slots of the call: rows of the buffer behind them are."""
+    K, S = 128, sum(counts)
+    dev, ref, tol = _case(counts, 20, K, N, "none", x4, False, seed=5)
+    x, xs = dev["x"] if x4 else (dev["x"], None)
+    cut, off = S - counts[-1] // 2 - 1, dev["offsets"]
+    slots = torch.arange(S, dtype=torch.int32, device="cuda")
+    for rows, T in ((slots, S), (None, cut)):
+        out = torch.full((S + 7, N), 77.0, dtype=BF, device="cuda")
+        B.moe_mx_gemm(x, xs, *dev["w"], None, None, off, rows, T, cut, K, N, len(counts), 0, out)
+        assert (out[cut:] == 77).all()
+    e = len(counts) - 1
+    w = [t[e:].contiguous() for t in dev["w"]]
+    out = torch.full((S + 7, N), 77.0, dtype=BF, device="cuda")
+    B.moe_mx_gemm(x, xs, *w, None, None, off[e:].clone(), None, S, S, K, N, 1, 0, out)
+    got, lo = out.double().cpu().numpy(), S - counts[e]
+    assert (np.abs(got[lo:S] - ref[lo:]) <= tol[lo:]).all() and (got[:lo] == 77).all() and (got[S:] == 77).all()
+
+
+@pytest.mark.parametrize("x4", [False, True])
+@pytest.mark.parametrize("counts,N", CORES)
+def test_product_of_offsets_that_are_none(x4, counts, N):
+    """Negative, decreasing and huge offsets: nothing outside the result's rows is written."""
+    K, S, E = 64, sum(counts), len(counts)
+    dev, *_ = _case(counts, 20, K, N, "none", x4, False, seed=6)
+    x, xs = dev["x"] if x4 else (dev["x"], None)
+    buf = torch.full((S + 128, N), 77.0, dtype=BF, device="cuda")
+    big = (1 << 31) - 1
+    for off in ([0] + [big] * E, [-1 - big] * E + [big], [S] + [0] * E, [-5] * E + [S], [big] * E + [0],
+                [S + 50] * E + [S + 90], [big - 3] * E + [big], [0, S, -S, big][:E] + [S] * (E + 1 - len([0, S, -S, big][:E]))):
+        print(off, flush=True)
+        off = torch.tensor(off, dtype=torch.int32, device="cuda")
+        B.moe_mx_gemm(x, xs, *dev["w"], None, None, off, None, S, S, K, N, E, 0, buf[64:64 + S])
+        torch.cuda.synchronize()
+        assert (buf[:64] == 77).all() and (buf[64 + S:] == 77).all()
