@@ -32,6 +32,8 @@
  *    16-byte aligned.
  *  - Calls that share output or workspace buffers must be ordered on one
  *    stream; concurrent calls on different streams must use disjoint buffers.
+ *  - Unless a call says otherwise, its outputs and its workspace overlap neither
+ *    its inputs nor each other.
  */
 #ifndef MOEBLAZE_H
 #define MOEBLAZE_H
@@ -438,7 +440,8 @@ int moe_mx_dequantize(const void* codes, const void* scales, int64_t R, int K, u
  * In:  x [T,K] bfloat16 (x_scales NULL), or codes [T,K/2] with x_scales [T,K/32]
  *      as moe_mx_quantize writes them; w, w3 [E,N,K/2] codes, w_scales, w3_scales
  *      [E,N,K/32] (w3 with MOE_GATED, else NULL); offsets [E+1], rows [S] int32.
- * Out: out [S,N] bfloat16. Rows at or behind offsets[E] are left as they were.
+ * Out: out [S,N] bfloat16, apart from every input (MOE_ERR_INVALID_ARG). Rows at or
+ * behind offsets[E] are left as they were.
  * Limits: K and N multiples of 64, N K < 2^33, E <= 256, S < 2^31, T < 2^31; rows
  * NULL: T == S. (Beyond an S N of about 2^36 a grid may not be launchable:
  * MOE_ERR_HIP.)

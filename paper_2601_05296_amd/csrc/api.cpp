@@ -558,6 +558,11 @@ int check_grads(const char* fn, const void* const* grads, const int64_t* sizes, 
     return MOE_OK;
 }
 
+bool overlap(const void* a, size_t na, const void* b, size_t nb) {
+    const uintptr_t p = reinterpret_cast<uintptr_t>(a), q = reinterpret_cast<uintptr_t>(b);
+    return p < q + nb && q < p + na;
+}
+
 // Among the tensors that a clip reads and writes, no written one may share memory with
 // another. O(n log n) on the host.
 int check_overlap(const char* fn, const void* const* grads, void* const* outs, const int64_t* sizes,
@@ -701,6 +706,15 @@ int moe_mx_gemm(const void* x, const void* x_scales, const void* w, const void* 
     OPT_PTR(x_scales); OPT_PTR(rows);
     FLAG_PTR(w3, flags & MOE_GATED, "MOE_GATED");
     FLAG_PTR(w3_scales, flags & MOE_GATED, "MOE_GATED");
+    // workgroups read x and the weights while others write
+    const size_t row = x_scales ? K / 2 : 2 * (size_t)K, mat = (size_t)E * N * (K / 2);
+    const struct { const void* p; size_t bytes; const char* name; } in[] = {
+        {x, T * row, "x"}, {x_scales, T * (size_t)(K / 32), "x_scales"}, {w, mat, "w"},
+        {w_scales, mat / 16, "w_scales"}, {w3, mat, "w3"}, {w3_scales, mat / 16, "w3_scales"},
+        {offsets, (E + 1) * sizeof *offsets, "offsets"}, {rows, S * sizeof *rows, "rows"}};
+    for (const auto& i : in)
+        if (i.p && overlap(i.p, i.bytes, out, (size_t)S * N * 2))
+            return fail(MOE_ERR_INVALID_ARG, "%s: out overlaps %s", fn, i.name);
     moe::MxArgs a{};
     a.x = x; a.xs = static_cast<const uint8_t*>(x_scales);
     a.w = static_cast<const uint8_t*>(w); a.ws = static_cast<const uint8_t*>(w_scales);

@@ -95,7 +95,7 @@ def product(x, w: MX, offsets, rows=None, w3: MX | None = None, act: str = "none
 
     ``x``: bfloat16 [T, K], or MX. ``w``, ``w3``: MX [E, N, K]. ``rows``: int32 [S], the
     row of x of each slot (expert_token_indices); None: slot s is row s. Returns ``out``
-    [S, N] bfloat16; rows at or behind offsets[E] are not written."""
+    [S, N] bfloat16 (no input's memory); rows at or behind offsets[E] are not written."""
     if stream is not None:
         with _on(stream):
             return product(x, w, offsets, rows, w3, act, out)

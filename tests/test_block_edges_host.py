@@ -47,3 +47,19 @@ def test_quantize_refuses_what_no_launch_covers():
     assert quant(1, (1 << 31) - 127, 32, B.MOE_F32) == B.MOE_ERR_UNSUPPORTED
     for rows in ((1 << 29) - 126, (1 << 29) - 2):
         assert quant(1, rows, 32, B.MOE_TRANSPOSED) == B.MOE_ERR_UNSUPPORTED and b"2^29 - 128" in lib.moe_last_error()
+
+
+def test_product_refuses_results_over_its_inputs():
+    lib = B.load_library()
+    far = 1 << 30
+
+    def gemm(x=far, xs=None, w=2 * far, ws=3 * far, w3=4 * far, ws3=5 * far, off=6 * far, rows=7 * far, out=FAKE):
+        return lib.moe_mx_gemm(x, xs, w, ws, w3, ws3, off, rows, 4, 8, 64, 128, 2, B.MOE_GATED, out, None)
+
+    # out 2048 bytes; x 512 (256 and 8 in 4 bits), weights 8192 and 512 each, offsets 12, rows 32
+    for name, size in (("x", 512), ("w", 8192), ("ws", 512), ("w3", 8192), ("ws3", 512), ("off", 12), ("rows", 32)):
+        what = {"ws": "w_scales", "ws3": "w3_scales", "off": "offsets"}.get(name, name)
+        for at in (FAKE, FAKE + 2032, FAKE - (size - 1) // 16 * 16):
+            assert gemm(**{name: at}) == B.MOE_ERR_INVALID_ARG, (name, at)
+            assert b"out overlaps " + what.encode() in lib.moe_last_error()
+    assert gemm(xs=FAKE + 16) == B.MOE_ERR_INVALID_ARG and b"x_scales" in lib.moe_last_error()

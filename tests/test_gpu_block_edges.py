@@ -190,3 +190,18 @@ def test_product_of_offsets_that_are_none(x4, counts, N):
         B.moe_mx_gemm(x, xs, *dev["w"], None, None, off, None, S, S, K, N, E, 0, buf[64:64 + S])
         torch.cuda.synchronize()
         assert (buf[:64] == 77).all() and (buf[64 + S:] == 77).all()
+
+
+def test_product_beside_its_inputs():
+    """Results right behind x in one buffer are taken, over x they are refused."""
+    K = N = 128
+    S = 40
+    dev, ref, tol = _case([S], 20, K, N, "none", False, False, seed=7)
+    buf = torch.zeros(2 * S, K, dtype=BF, device="cuda")
+    buf[:S] = dev["x"]
+    dev["x"] = buf[:S]
+    for out in (buf[:S], buf[S - 1:2 * S - 1]):
+        with pytest.raises(B.MoEError, match="out overlaps x"):
+            mx.product(**dev, out=out)
+    mx.product(**dev, out=buf[S:])
+    assert (np.abs(buf[S:].double().cpu().numpy() - ref) <= tol).all()
