@@ -205,3 +205,28 @@ def test_product_beside_its_inputs():
             mx.product(**dev, out=out)
     mx.product(**dev, out=buf[S:])
     assert (np.abs(buf[S:].double().cpu().numpy() - ref) <= tol).all()
+
+
+def test_calls_of_the_binding_are_those_of_the_modules():
+    """One function of the binding for each entry point, on the caller's own buffers."""
+    ts = [torch.randn(1000, device="cuda"), torch.randn(77, device="cuda").to(BF)]
+    tl = B.TensorList(ts)
+    norm, sumsq = torch.empty((), device="cuda"), torch.empty((), dtype=torch.float64, device="cuda")
+    n = B.moe_grad_norm_workspace_size(tl.n)
+    ws = torch.empty(n, dtype=torch.uint8, device="cuda")
+    B.moe_grad_norm(tl, sumsq, norm, ws, n)
+    want = grads.norm(ts)
+    assert torch.equal(norm, want[0]) and torch.equal(sumsq, want[1])
+    q = mx.quantize(ts[0][:960].reshape(10, 96))
+    for dt, fl in ((BF, B.MOE_BF16), (F32, B.MOE_F32)):
+        out = torch.empty(10, 96, dtype=dt, device="cuda")
+        B.moe_mx_dequantize(q.codes, q.scales, 10, 96, fl, out)
+        assert torch.equal(out, mx.dequantize(q, dt))
+    with pytest.raises(ValueError, match="workspace"):
+        B.moe_grad_norm(tl, sumsq, norm, ws[:8], n)
+    with pytest.raises(ValueError, match="sumsq: dtype"):
+        B.moe_grad_norm(tl, norm, norm, ws, n)
+    with pytest.raises(ValueError, match="out: dtype"):
+        B.moe_mx_dequantize(q.codes, q.scales, 10, 96, B.MOE_F32, torch.empty(960, dtype=BF, device="cuda"))
+    with pytest.raises(ValueError, match="scales: 20 elements"):
+        B.moe_mx_dequantize(q.codes, q.scales[:, :2].contiguous(), 10, 96, B.MOE_BF16, out)
