@@ -5,7 +5,8 @@ One block, x its residual stream (p = post_norm(y) * w_post, or y without a post
   n = rms_norm(x) * w_pre;  y = layer(n);  x' = res_scale * x + gate * p
 ``norm_forward`` does a block's last line and the next block's first in one pass;
 ``forward`` and ``backward`` chain a list of blocks with it, ``infer`` serves the same
-blocks with their experts in 4 bits (mx.py).
+blocks with their experts in 4 bits (mx.py). Rows of the norms: d a multiple of 8, at most
+8192, which is a block's limit where the layer has none.
 """
 from __future__ import annotations
 
@@ -198,7 +199,8 @@ def backward(blocks, saved: Saved, dr, stream=None):
 
 
 def infer(blocks, x, eps: float = 1e-6, rows: str = "bf16", stream=None):
-    """x through the blocks with their 4-bit ``experts`` (mx.forward); nothing is kept."""
+    """x (bfloat16) through the blocks with their 4-bit ``experts`` (mx.forward); nothing is
+    kept."""
     blocks = list(blocks)
     if not blocks:
         raise ValueError("no blocks")

@@ -82,8 +82,10 @@ __device__ __forceinline__ bool inside(const Args& a, SlotTile& t) {
 // Loads straight into registers in the layout of the matrix instructions, 16 rows a load
 // and a scale byte with each, reached 3.3 TB/s: the address unit takes a cycle for every
 // line that four neighbouring lanes touch. Copies into LDS with eight lanes to a line cut
-// that to a quarter, and the scales come for CHUNK blocks of K at a time, 16 bytes a load:
-// 5.2 TB/s (one token's gated product at K = 4096, N = 14336, two experts: 41 -> 24 us).
+// that to a quarter, and the scales come for CHUNK blocks of K at a time, 16 bytes a load
+// (one token's gated product at K = 4096, N = 14336, two experts: 41 -> 24 us, of it 22.4 in
+// the kernel with the same 125 MB of weights pass after pass, which the last-level cache
+// holds; behind other layers' weights, from HBM, 25.2, 5.0 TB/s).
 __device__ __constant__ uint4 g_zero16 = {0u, 0u, 0u, 0u};
 
 template <int BM_, int BN_, int WN_, int WK_, int GROUPS_, int NB_, bool X4_, int NST_, int CHUNK_>
@@ -304,11 +306,11 @@ mx_stream(const Args a) {
 
 // ---- tile core --------------------------------------------------------------------------
 // Measured: 4-bit rows 4096 -> 14336 gated, eight experts, 3554 slots (444 rows each in tiles
-// of 256) 289 us, 2.89 PFLOP/s; 16384 slots 1137, 3.38, where a loop of the scaled instruction
-// alone reaches 4.5. bfloat16 rows 2048 -> 1408 gated, 64 experts,
-// 98304 slots 975 to 1030 us, 1.1 to 1.16 PFLOP/s; 8192 x 8192 x 8192 1.28. About 12 (8) us of
-// a tile's time, its first copies and its results, run beside no matrix instruction: one
-// workgroup a CU.
+// of 256) 287 to 291 us, 2.9 PFLOP/s; 16384 slots 1137, 3.38, where a loop of the scaled
+// instruction alone reaches 7.0 on random values (9.6 on zeros: power bounds it). bfloat16 rows
+// 2048 -> 1408 gated, 64 experts, 98304 slots 975 to 1030 us, 1.1 to 1.16 PFLOP/s;
+// 8192 x 8192 x 8192 1.28, a loop of its instruction 1.8 (2.5). About 12 (8) us of a tile's
+// time, its first copies and its results, run beside no matrix instruction: one workgroup a CU.
 // BM x BN outputs of NB weights, WM x WN waves of 32 x 32 fragments. A slice is 64 values of
 // K with bfloat16 rows (128-byte rows of x, 32-byte rows of codes), 256 with 4-bit rows
 // (128-byte rows of either: whole lines take 40% fewer requests to L2 than slices of 128 do).
@@ -825,26 +827,35 @@ hipError_t pick(const MxArgs& m, const Args& a, hipStream_t st) {
     // The largest tile that the rows fill and that still gives two thirds of the CUs one: its
     // operands are used most often, but a workgroup takes as long on an idle chip as on a full
     // one (K = 4096, bfloat16 rows, one weight, tiles of 256, 128, 64 and 32 rows: 79, 49, 38, 16).
-    // K -> N, rows of each of E experts; 256, 128, 64, 32 rows a tile:
-    //                                        bfloat16 rows, one weight    4-bit rows, gated
-    //   4096 -> 14336   8 x  32                   -  118  76.2  62.7        139   115   105  99.3
-    //                   8 x  64                 188  125  83.0  92.0        145   122   116   124
-    //                   8 x 128                 198  133   145    -         154   136   175   199
-    //                   8 x 512                 412  459   517    -         290   397   621   678
-    //   14336 -> 4096   8 x 128                 262  216   155    -         132   122   163   213
-    //                   8 x 256                 299  243   261    -         149   196   289   381
-    //   4096 -> 4096    2 x 128                79.0 49.3  38.8  17.5       27.0  22.2  18.2  15.3
-    //                   2 x 256                78.8 49.7  39.9  25.1       29.0  22.7  20.4  28.0
-    //                   2 x 1024               85.9 65.8  74.3  89.5       40.7  51.2  75.3  82.1
-    //   2880 -> 2880    4 x 512                59.6 40.9  45.6  52.8       31.6  42.1  48.7  61.4
+    // 256, 128, 64, 32 rows a tile, K -> N, E experts of so many rows:
+    //                              bfloat16 rows: one weight,       gated         4-bit rows: one weight,         gated
+    //   4096 -> 14336  8 x  32   168  108 68.1 46.5   360  239  154  110   60.3 46.3 42.8 44.1    143  115  104 97.5
+    //                  8 x  64   177  116 78.5 80.9   368  247  165  178   68.8 55.2 48.7 52.6    140  119  114  124
+    //                  8 x 128   200  132  143  158   390  258  270  318   80.3 66.4 91.3 97.2    152  136  174  199
+    //                  8 x 512   422  465  524  628   754  918 1024 1223    174  215  330  360    292  400  626  685
+    //   14336 -> 4096  8 x 128   265  222  156  158   349  254  273  309   91.3 76.4 67.4 94.5    127  121  163  215
+    //                  8 x 256   298  238  257  300   373  470  505  586    118 94.5  143  177    148  191  289  385
+    //   4096 -> 4096   2 x 128  79.1 49.7 38.8 16.0  75.7 50.3 37.3 23.4   28.4 18.2 14.5 10.6   25.8 21.9 17.8 15.0
+    //                  2 x 256  79.8 50.4 39.4 23.9  77.2 50.9 41.4 43.2   28.9 18.8 15.2 14.5   28.3 22.2 19.6 27.4
+    //                  2 x 1024 83.4 66.3 73.5 90.7   108  126  139  174   32.9 27.5 38.9 43.8   39.3 48.9 73.2 81.0
+    //   2880 -> 2880   4 x 512  60.4 41.8 45.6 51.5  62.8 80.3 76.0  102   29.0 22.0 31.3 32.1   30.2 41.3 48.1 60.2
+    //   2048 -> 1408   64 x 48  89.1 59.7 36.1 37.7   135 90.0 58.0 66.1   37.6 30.6 25.3 22.6   52.7 41.5 37.4 38.4
+    //                  64 x 96  93.6 61.7 57.8 54.6   141 94.6  100 99.8   41.8 31.6 34.6 31.1   55.8 44.9 60.7 52.2
+    //                  64 x 192  101  103 89.5  106   161  195  160  211   46.5 48.1 55.1 56.4   65.0 82.5 90.8 96.1
+    // The rule takes the fastest of these, or one within 5% of it, in 47 of the 52; in the others
+    // it loses 8 to 17% (2 x 128 rows, 4-bit gated: 17.6 of 64 rows against 15.0 of 32). The host
+    // knows the experts' mean alone, and under a skewed routing no expert may have it: gated
+    // products of 16 to 8192 tokens by four layers' shapes, experts drawn by a Zipf law of 1.2,
+    // lose more than 6% in 5 of 40 cases, the most in 2048 -> 1408, bfloat16, 1777 tokens of 64
+    // experts (mean 167, largest 1632): 204 of 256 rows against 158 of 64.
     auto fills = [&](int bm, int bn) {
         return (double)active * std::ceil(rows / bm) * ((m.N + bn - 1) / bn) * 3.0 >= 2.0 * 256.0;
     };
     if (rows > 128 && fills(256, BN)) return tile<TCfg<256, BN, 2, 4, NB, X4, NST>>(m, a, st);
     if (rows > 64 && fills(128, BN)) return tile<TCfg<128, BN, 2, 4, NB, X4, NST>>(m, a, st);
     // With 4-bit rows half as many columns, twice the workgroups, where 64 rows: 4096 -> 14336,
-    // 8 x 48 rows 56.9, 64.6; 2048 -> 1408 gated, 64 x 48 rows 47.2, 53.7; bfloat16 rows, which
-    // four waves side by side convert once each: 98.3, 80.4; 70.4, 66.2.
+    // 8 x 48 rows 48.4, 57.0; 2048 -> 1408 gated, 64 x 48 rows 37.7, 43.7. bfloat16 rows, for
+    // which four waves side by side convert the weights once each: 93.4, 79.7; 63.6, 60.2.
     constexpr int BN64 = X4 ? BN / 2 : BN;
     if (rows > 32 && fills(64, BN64)) {
         if constexpr (X4) return tile<TCfg<64, BN64, 2, 2, NB, X4, NST>>(m, a, st);

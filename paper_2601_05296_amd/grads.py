@@ -1,5 +1,6 @@
-"""The global norm of gradients, and clipping by it, over any list of tensors: the
-layer's own gradients are float32, a model's others may be bfloat16."""
+"""The global norm of gradients, and clipping by it, over any list of contiguous tensors,
+which may start anywhere: the layer's own gradients are float32, a model's others may be
+bfloat16."""
 from __future__ import annotations
 
 import torch

@@ -6,8 +6,9 @@ byte for each 32 values along the axis that a product sums over, a weight takes 
 a byte instead of two. ``quantize_experts`` makes the layer's weights ready once;
 ``forward`` is ``layer.forward`` on them: the same router, index build and combine, the
 experts' products by moe_mx_gemm, on bfloat16 rows or (``rows="mx"``) on rows quantised
-to 4 bits themselves, which the scaled matrix instructions multiply at four times the
-bfloat16 rate. Inference only: the weights have no gradient.
+to 4 bits themselves, which the scaled matrix instructions multiply four times as fast as
+bfloat16 ones (3.8 times in loops of either alone; whole products 2.1 to 2.8 times where
+an expert has hundreds of rows). Inference only: the weights have no gradient.
 """
 from __future__ import annotations
 
@@ -43,7 +44,8 @@ class MXExperts(NamedTuple):
 
 def quantize(x, transpose: bool = False, stream=None) -> MX:
     """``x`` [..., R, K] (bfloat16 or float32) in 4 bits, with a scale for each 32 values
-    along K; with ``transpose`` of [..., K, R], whose result is laid out [..., R, K]."""
+    along K; with ``transpose`` of [..., K, R] (R even), whose result is laid out
+    [..., R, K]."""
     if stream is not None:
         with _on(stream):
             return quantize(x, transpose)
